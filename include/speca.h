@@ -82,6 +82,7 @@ extern "C" {
 #define SPECA_STATUS_TOO_MANY    16   /* a sequence has more than dims.max_nodes nodes             */
 #define SPECA_STATUS_TIMEOUT     32   /* a bounded device-side wait gave up                        */
 #define SPECA_STATUS_BAD_DEPTH   64   /* depth[] given and inconsistent with parent[]              */
+#define SPECA_STATUS_BAD_PAGE   128   /* a cache length or page index out of range, or a page copied onto twice or while read */
 
 /* verification routes (dims.route) */
 #define SPECA_ROUTE_AUTO        0   /* library picks                                              */
@@ -358,6 +359,87 @@ int speca_verify_tree_noalloc(const speca_dims *dims, const float *S0,
                               const int32_t *parent, const int32_t *depth_or_null,
                               float *o, float *u_or_null,
                               int32_t *status_word, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * Attention layers of a hybrid stack.  Between its gated-delta-rule layers such a stack keeps layers with softmax
+ * attention, whose state is a cache of keys and values.  A speculative round goes through them as it goes through the
+ * others: the draft's keys and values are records, packed like q, k, v above; verification reads the committed cache and
+ * never writes it; commit appends the records of the accepted path.  (The paper has no counterpart.)
+ *
+ *      q, o              bf16   [L][T][heads][d_head]
+ *      k, v              bf16   [L][T][kv_heads][d_head]       query head h belongs to key head h / (heads / kv_heads)
+ *      k_cache, v_cache  bf16   [L][n_pages][kv_heads][page_size][d_head]
+ *      page_table        int32  [B][max_pages]   row i of sequence b: page page_table[b][i / page_size], row i % page_size
+ *      kv_len            int32  [B]              committed rows of every sequence (0 allowed)
+ *
+ * Entries of page_table past a sequence's length, and rows of its last page past it, are never used, whatever they hold.
+ * Pages may be shared between sequences: only speca_commit_kv and speca_copy_pages write them.  Which pages a sequence
+ * holds, who shares them and which are free is the caller's bookkeeping, as all memory is.
+ *
+ * parent_or_null == NULL: every sequence is a chain (a prompt, or one token); max_nodes is then 1..8192, with a parent
+ * array 1..1024.  total_nodes is at most batch * max_nodes.  A sequence with bad topology, a bad length or a bad page in
+ * its length is reported in *status_word and skipped: its outputs, or its part of the cache, stay untouched. */
+typedef struct speca_attn_dims {
+    int32_t n_layers;    /* L >= 1                                                    */
+    int32_t batch;       /* B >= 1                                                    */
+    int32_t heads;       /* query heads, a multiple of kv_heads                       */
+    int32_t kv_heads;    /* key and value heads >= 1                                  */
+    int32_t d_head;      /* 64, 128 or 256                                            */
+    float   scale;       /* softmax(scale * q k^T), > 0; usually d_head ^ -1/2        */
+    int32_t max_nodes;   /* draft nodes (or prompt tokens) per sequence and call      */
+    int32_t page_size;   /* rows of a page: 16, 32, 64, 128 or 256                    */
+    int32_t n_pages;     /* pages of the pool                                         */
+    int32_t max_pages;   /* width of a page_table row                                 */
+} speca_attn_dims;
+
+/* Norm and rotation of queries and keys in one pass.  Per head, with p = kv_len[b] + (depth of the node) - 1:
+ *      y = x * rsqrt(mean(x^2) + eps) * weight            weight float [L][d_head]; NULL: y = x
+ *      (a, b) <- rope_scale * (a cos - b sin, a sin + b cos)   of the angle p * inv_freq[j], j < rot_dim / 2
+ * on the pairs (y[j], y[j + rot_dim/2]), or (y[2j], y[2j+1]) where interleaved != 0; y[rot_dim..] is not rotated.
+ * inv_freq float [rot_dim / 2]: scaling for long contexts is in it and in rope_scale.  rot_dim is a multiple of 16, at
+ * most d_head; 0 rotates nothing.  Angles are formed in 64 bits, the rest in fp32, one rounding to bf16 at the end.
+ * q and k may be slices of wider rows: strides are in elements, multiples of 8, between layers and between tokens
+ * (heads of a token are dense).  q_out and k_out are dense and alias no input. */
+int speca_norm_rope(const speca_attn_dims *dims,
+                    const uint16_t *q, int64_t q_layer_stride, int64_t q_token_stride,
+                    const uint16_t *k, int64_t k_layer_stride, int64_t k_token_stride,
+                    const float *q_weight_or_null, const float *k_weight_or_null, float eps,
+                    const float *inv_freq, int32_t rot_dim, int32_t interleaved, float rope_scale,
+                    const int32_t *node_offsets, int32_t total_nodes, const int32_t *parent_or_null,
+                    const int32_t *kv_len, uint16_t *q_out, uint16_t *k_out,
+                    int32_t *status_word, void *stream);
+
+/* Verification by an attention layer: node t attends the committed rows 0 .. kv_len[b]-1 of its sequence, its ancestors in
+ * the draft and itself.  Scores, softmax and sums in fp32; weights are rounded to bf16 for the product with v, and o
+ * once at the end.  A key or value that is not finite reaches the nodes that attend it and no others. */
+size_t speca_attn_workspace_bytes(const speca_attn_dims *dims);
+int speca_attend_tree(const speca_attn_dims *dims, const uint16_t *q, const uint16_t *k, const uint16_t *v,
+                      const int32_t *node_offsets, int32_t total_nodes, const int32_t *parent_or_null,
+                      const uint16_t *k_cache, const uint16_t *v_cache,
+                      const int32_t *page_table, const int32_t *kv_len, uint16_t *o,
+                      void *workspace, size_t workspace_bytes, int32_t *status_word, void *stream);
+
+/* Commit of the cache: the k, v records of the accepted nodes path_idx[b][0..path_len[b]) (as speca_greedy_accept writes
+ * them, rows of max_depth entries, 1..16) become rows kv_len[b] .. of the sequence, and kv_len_out[b] = kv_len[b] +
+ * path_len[b].  path_idx == path_len == NULL appends all nodes of every sequence in order (a prompt; parent_or_null and
+ * max_depth are then not looked at).  16-bit patterns are copied: the result is exact.  The page table must already hold
+ * the pages of the new rows.  If parent_or_null is given the path is checked to be a chain of parent links from a root.
+ * A skipped sequence keeps its length.  kv_len_out may be kv_len itself, and must not overlap it otherwise.  The row of one
+ * sequence's append must not be another's: a page that is written here belongs to one sequence. */
+int speca_commit_kv(const speca_attn_dims *dims, uint16_t *k_cache, uint16_t *v_cache,
+                    const int32_t *page_table, const int32_t *kv_len,
+                    const uint16_t *k, const uint16_t *v, const int32_t *node_offsets, int32_t total_nodes,
+                    const int32_t *parent_or_null, int32_t max_depth,
+                    const int32_t *path_idx_or_null, const int32_t *path_len_or_null,
+                    int32_t *kv_len_out, int32_t *status_word, void *stream);
+
+/* Copies page src[i] onto page dst[i], i < n_copies, in every layer, keys and values: the page a forked sequence goes on
+ * writing (full pages need no copy, they are shared).  src, dst int32 [n_copies], device.  A source may be named often.
+ * Copies are unordered, so a pair whose dst is out of range, is another pair's dst, or is any pair's src is reported
+ * (STATUS_BAD_PAGE) and not made, and so is one whose src is out of range; the others are.  Of dims only n_layers,
+ * kv_heads, d_head, page_size and n_pages matter. */
+int speca_copy_pages(const speca_attn_dims *dims, uint16_t *k_cache, uint16_t *v_cache,
+                     const int32_t *src, const int32_t *dst, int32_t n_copies, int32_t *status_word, void *stream);
 
 #ifdef __cplusplus
 }

@@ -30,7 +30,7 @@ MARSHAL_PATH = os.path.join(_HERE, f"speca_marshal.{sysconfig.get_config_var('SO
 
 OK = 0
 STATUS_BAD_PARENT, STATUS_BAD_OFFSETS, STATUS_BAD_PATH, STATUS_TOO_DEEP = 1, 2, 4, 8
-STATUS_TOO_MANY, STATUS_TIMEOUT, STATUS_BAD_DEPTH = 16, 32, 64
+STATUS_TOO_MANY, STATUS_TIMEOUT, STATUS_BAD_DEPTH, STATUS_BAD_PAGE = 16, 32, 64, 128
 ROUTE_AUTO, ROUTE_SERIAL, ROUTE_FACTORIZED, ROUTE_TF32, ROUTE_EFFECTIVE = 0, 1, 2, 3, 4
 RULE_GATED_DELTA, RULE_GATED_NO_ERASE = 0, 1
 
@@ -38,7 +38,8 @@ EXPORTS = ["speca_version", "speca_strerror", "speca_workspace_bytes", "speca_de
            "speca_verify_chain", "speca_verify_tree", "speca_greedy_accept", "speca_commit",
            "speca_verify_tree_noalloc", "speca_commit_verify_tree", "speca_commit_conv",
            "speca_tree_mask_to_parent", "speca_prune_tree", "speca_stochastic_accept",
-           "speca_chain_decompose"]
+           "speca_chain_decompose", "speca_norm_rope", "speca_attn_workspace_bytes", "speca_attend_tree",
+           "speca_commit_kv", "speca_copy_pages"]
 NOALLOC_MAX_BATCH, NOALLOC_MAX_NODES = 256, 16384
 
 
@@ -69,6 +70,33 @@ class Dims:
     def c(self) -> _Dims:
         return _Dims(self.n_layers, self.batch, self.heads, self.d_k, self.d_v, self.scale,
                      self.max_depth, self.max_nodes, self.route, self.rule)
+
+
+class _AttnDims(ctypes.Structure):
+    _fields_ = [("n_layers", ctypes.c_int32), ("batch", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("d_head", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("max_nodes", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32)]
+
+
+@dataclass
+class AttnDims:
+    """Shape of the attention layers' calls (speca_attn_dims): ``heads`` query heads over ``kv_heads`` key heads of width
+    ``d_head``, a pool of ``n_pages`` pages of ``page_size`` rows, ``max_pages`` page-table entries a sequence."""
+    n_layers: int
+    batch: int
+    heads: int
+    kv_heads: int
+    d_head: int
+    scale: float = 1.0
+    max_nodes: int = 64
+    page_size: int = 16
+    n_pages: int = 1
+    max_pages: int = 1
+
+    def c(self) -> _AttnDims:
+        return _AttnDims(self.n_layers, self.batch, self.heads, self.kv_heads, self.d_head, self.scale, self.max_nodes,
+                         self.page_size, self.n_pages, self.max_pages)
 
 
 _lib = None
@@ -106,6 +134,15 @@ def lib() -> ctypes.CDLL:
         L.speca_chain_decompose.argtypes = [i32, i32] + [vp] * 6
         L.speca_chain_decompose.restype = ctypes.c_int
         L.speca_stochastic_accept.restype = ctypes.c_int
+        ap, i64, f32 = ctypes.POINTER(_AttnDims), ctypes.c_int64, ctypes.c_float
+        L.speca_norm_rope.argtypes = ([ap, vp, i64, i64, vp, i64, i64, vp, vp, f32, vp, i32, i32, f32, vp, i32] + [vp] * 6)
+        L.speca_attn_workspace_bytes.argtypes = [ap]
+        L.speca_attn_workspace_bytes.restype = sz
+        L.speca_attend_tree.argtypes = [ap] + [vp] * 4 + [i32] + [vp] * 7 + [sz, vp, vp]
+        L.speca_commit_kv.argtypes = [ap] + [vp] * 7 + [i32, vp, i32] + [vp] * 5
+        L.speca_copy_pages.argtypes = [ap] + [vp] * 4 + [i32, vp, vp]
+        for name in ("speca_norm_rope", "speca_attend_tree", "speca_commit_kv", "speca_copy_pages"):
+            getattr(L, name).restype = ctypes.c_int
         for name in ("speca_decode_step", "speca_verify_chain", "speca_verify_tree", "speca_greedy_accept",
                      "speca_commit", "speca_verify_tree_noalloc", "speca_commit_verify_tree", "speca_commit_conv"):
             getattr(L, name).restype = ctypes.c_int
@@ -388,3 +425,112 @@ def chain_decompose(max_nodes: int, node_offsets, parent, chain_head, n_chains, 
                                      _ptr(parent, i32, (T,), "parent"), _ptr(chain_head, i32, (T,), "chain_head"),
                                      _ptr(n_chains, i32, (B,), "n_chains"), _ptr(status, i32, (1,), "status"), _stream())
     _check(rc, "speca_chain_decompose")
+
+
+def attn_workspace_bytes(dims: AttnDims) -> int:
+    d = dims.c()
+    return int(lib().speca_attn_workspace_bytes(ctypes.byref(d)))
+
+
+def alloc_attn_workspace(dims: AttnDims, device="cuda") -> torch.Tensor:
+    return torch.empty(attn_workspace_bytes(dims), dtype=torch.uint8, device=device)
+
+
+def _here(*tensors) -> None:
+    """The kernels run on the current device and its current stream: tensors of another device are refused."""
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device.index != torch.cuda.current_device():
+            raise SpecaError(f"a tensor on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _heads(t, shape, name):
+    """Address and layer and token strides of [L, T, H, d] whose heads are dense in a token."""
+    if not t.is_cuda or t.dtype != torch.bfloat16 or tuple(t.shape) != tuple(shape):
+        raise SpecaError(f"{name}: need a CUDA tensor of dtype {torch.bfloat16} and shape {tuple(shape)}, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
+    if t.stride(3) != 1 or (shape[2] > 1 and t.stride(2) != shape[3]):
+        raise SpecaError(f"{name}: the heads of a token must be dense, got strides {t.stride()}")
+    return [ctypes.c_void_p(t.data_ptr()), t.stride(0), t.stride(1)]
+
+
+def _caches(dims, k_cache, v_cache):
+    shape = (dims.n_layers, dims.n_pages, dims.kv_heads, dims.page_size, dims.d_head)
+    return [_ptr(k_cache, torch.bfloat16, shape, "k_cache"), _ptr(v_cache, torch.bfloat16, shape, "v_cache")]
+
+
+def norm_rope(dims: AttnDims, q, k, q_weight, k_weight, eps: float, inv_freq, rot_dim: int, interleaved: bool,
+              rope_scale: float, node_offsets, total_nodes, parent, kv_len, q_out, k_out, status) -> None:
+    """speca_norm_rope: per-head RMS norm (weights fp32 [L,d], or None) and rotation by kv_len + depth - 1 of the draft's
+    queries and keys.  q and k may be slices of a fused projection; ``parent`` None: chains."""
+    rc = (_native or _load_native()).norm_rope(dims, q, k, q_weight, k_weight, eps, inv_freq, rot_dim, interleaved, rope_scale,
+                                               node_offsets, total_nodes, parent, kv_len, q_out, k_out, status)
+    if rc is not None:
+        return _check(rc, "speca_norm_rope")
+    _here(q, k, q_weight, k_weight, inv_freq, node_offsets, parent, kv_len, q_out, k_out, status)
+    L, B, H, K, D, T = dims.n_layers, dims.batch, dims.heads, dims.kv_heads, dims.d_head, int(total_nodes)
+    i32, f32, bf16 = torch.int32, torch.float32, torch.bfloat16
+    d = dims.c()
+    rc = lib().speca_norm_rope(
+        ctypes.byref(d), *_heads(q, (L, T, H, D), "q"), *_heads(k, (L, T, K, D), "k"),
+        _ptr(q_weight, f32, (L, D), "q_weight"), _ptr(k_weight, f32, (L, D), "k_weight"), float(eps),
+        _ptr(inv_freq, f32, (int(rot_dim) // 2,), "inv_freq"), int(rot_dim), int(bool(interleaved)), float(rope_scale),
+        _ptr(node_offsets, i32, (B + 1,), "node_offsets"), T, _ptr(parent, i32, (T,), "parent"),
+        _ptr(kv_len, i32, (B,), "kv_len"), _ptr(q_out, bf16, (L, T, H, D), "q_out"),
+        _ptr(k_out, bf16, (L, T, K, D), "k_out"), _ptr(status, i32, (1,), "status"), _stream())
+    _check(rc, "speca_norm_rope")
+
+
+def attend_tree(dims: AttnDims, q, k, v, node_offsets, total_nodes, parent, k_cache, v_cache, page_table, kv_len, o,
+                workspace, status) -> None:
+    """speca_attend_tree: every draft node attends the committed rows of the paged cache, its ancestors and itself."""
+    rc = (_native or _load_native()).attend_tree(dims, q, k, v, node_offsets, total_nodes, parent, k_cache, v_cache, page_table,
+                                                 kv_len, o, workspace, status)
+    if rc is not None:
+        return _check(rc, "speca_attend_tree")
+    _here(q, k, v, node_offsets, parent, k_cache, v_cache, page_table, kv_len, o, workspace, status)
+    L, B, H, K, D, T = dims.n_layers, dims.batch, dims.heads, dims.kv_heads, dims.d_head, int(total_nodes)
+    i32, bf16 = torch.int32, torch.bfloat16
+    d = dims.c()
+    rc = lib().speca_attend_tree(
+        ctypes.byref(d), _ptr(q, bf16, (L, T, H, D), "q"), _ptr(k, bf16, (L, T, K, D), "k"), _ptr(v, bf16, (L, T, K, D), "v"),
+        _ptr(node_offsets, i32, (B + 1,), "node_offsets"), T, _ptr(parent, i32, (T,), "parent"),
+        *_caches(dims, k_cache, v_cache), _ptr(page_table, i32, (B, dims.max_pages), "page_table"),
+        _ptr(kv_len, i32, (B,), "kv_len"), _ptr(o, bf16, (L, T, H, D), "o"),
+        _ptr(workspace, torch.uint8, None, "workspace"), workspace.numel(), _ptr(status, i32, (1,), "status"), _stream())
+    _check(rc, "speca_attend_tree")
+
+
+def commit_kv(dims: AttnDims, k_cache, v_cache, page_table, kv_len, k, v, node_offsets, total_nodes, parent, path_idx,
+              path_len, kv_len_out, status) -> None:
+    """speca_commit_kv: append the k, v records of the accepted paths (None: of every node) to the cache's pages;
+    ``kv_len_out`` may be ``kv_len``."""
+    rc = (_native or _load_native()).commit_kv(dims, k_cache, v_cache, page_table, kv_len, k, v, node_offsets, total_nodes,
+                                               parent, path_idx, path_len, kv_len_out, status)
+    if rc is not None:
+        return _check(rc, "speca_commit_kv")
+    _here(k_cache, v_cache, page_table, kv_len, k, v, node_offsets, parent, path_idx, path_len, kv_len_out, status)
+    L, B, K, D, T = dims.n_layers, dims.batch, dims.kv_heads, dims.d_head, int(total_nodes)
+    i32, bf16 = torch.int32, torch.bfloat16
+    depth = 0 if path_idx is None else int(path_idx.shape[1])
+    d = dims.c()
+    rc = lib().speca_commit_kv(
+        ctypes.byref(d), *_caches(dims, k_cache, v_cache), _ptr(page_table, i32, (B, dims.max_pages), "page_table"),
+        _ptr(kv_len, i32, (B,), "kv_len"), _ptr(k, bf16, (L, T, K, D), "k"), _ptr(v, bf16, (L, T, K, D), "v"),
+        _ptr(node_offsets, i32, (B + 1,), "node_offsets"), T, _ptr(parent, i32, (T,), "parent"), depth,
+        _ptr(path_idx, i32, (B, depth), "path_idx"), _ptr(path_len, i32, (B,), "path_len"),
+        _ptr(kv_len_out, i32, (B,), "kv_len_out"), _ptr(status, i32, (1,), "status"), _stream())
+    _check(rc, "speca_commit_kv")
+
+
+def copy_pages(dims: AttnDims, k_cache, v_cache, src, dst, status) -> None:
+    """speca_copy_pages: page src[i] onto page dst[i] in every layer, keys and values (what a fork goes on writing)."""
+    rc = (_native or _load_native()).copy_pages(dims, k_cache, v_cache, src, dst, status)
+    if rc is not None:
+        return _check(rc, "speca_copy_pages")
+    _here(k_cache, v_cache, src, dst, status)
+    i32 = torch.int32
+    n = src.numel()
+    d = dims.c()
+    rc = lib().speca_copy_pages(ctypes.byref(d), *_caches(dims, k_cache, v_cache), _ptr(src, i32, (n,), "src"),
+                                _ptr(dst, i32, (n,), "dst"), n, _ptr(status, i32, (1,), "status"), _stream())
+    _check(rc, "speca_copy_pages")

@@ -1,6 +1,7 @@
 // extern "C" entry points of libspeca: argument validation and kernel dispatch only.
 #include <atomic>
 
+#include "attn.cuh"
 #include "speca_common.cuh"
 
 using namespace speca;
@@ -32,6 +33,42 @@ Params base_params(const speca_dims *d, int32_t total_nodes)
     p.no_erase = d->rule == SPECA_RULE_GATED_NO_ERASE;
     return p;
 }
+
+int check_attn_dims(const speca_attn_dims *d)
+{
+    if (d == nullptr) return SPECA_ERR_NULL;
+    if (d->n_layers < 1 || d->batch < 1 || d->heads < 1 || d->kv_heads < 1) return SPECA_ERR_RANGE;
+    if (d->n_pages < 1 || d->max_pages < 1 || d->max_nodes < 1 || d->max_nodes > kAttnMaxChain) return SPECA_ERR_RANGE;
+    if (d->heads % d->kv_heads != 0) return SPECA_ERR_UNSUPPORTED;
+    if (d->d_head != 64 && d->d_head != 128 && d->d_head != 256) return SPECA_ERR_UNSUPPORTED;
+    if (d->page_size < 16 || d->page_size > 256 || (d->page_size & (d->page_size - 1)) != 0) return SPECA_ERR_UNSUPPORTED;
+    // rows of the pool are TMA coordinates, head rows of a token and rows of a sequence 32-bit numbers
+    if (d->heads > 65536 || d->n_layers > 65536 || d->batch > (1 << 24)) return SPECA_ERR_RANGE;
+    const double rows = double(d->n_layers) * d->n_pages * d->kv_heads * d->page_size;
+    if (rows > 2147483647.0 || 1LL * d->max_pages * d->page_size > 0x7fffffffLL) return SPECA_ERR_RANGE;
+    return SPECA_OK;
+}
+
+// the part of a draft that every call over packed nodes checks
+int check_attn_draft(const speca_attn_dims *d, int32_t total_nodes, const int32_t *parent)
+{
+    if (total_nodes < 0 || 1LL * total_nodes > 1LL * d->batch * d->max_nodes) return SPECA_ERR_RANGE;
+    if (parent != nullptr && d->max_nodes > kAttnMaxTree) return SPECA_ERR_RANGE;
+    if (1LL * d->n_layers * total_nodes > 0x7fffffffLL) return SPECA_ERR_RANGE;
+    return SPECA_OK;
+}
+
+AttnParams attn_params(const speca_attn_dims *d, int32_t total_nodes)
+{
+    AttnParams p{};
+    p.L = d->n_layers; p.B = d->batch; p.H = d->heads; p.HK = d->kv_heads; p.T = total_nodes;
+    p.scale = d->scale; p.max_nodes = d->max_nodes; p.n_pages = d->n_pages; p.max_pages = d->max_pages;
+    for (p.page_shift = 4; (1 << p.page_shift) < d->page_size;) ++p.page_shift;
+    return p;
+}
+
+inline const __nv_bfloat16 *bf(const uint16_t *x) { return reinterpret_cast<const __nv_bfloat16 *>(x); }
+inline __nv_bfloat16 *bf(uint16_t *x) { return reinterpret_cast<__nv_bfloat16 *>(x); }
 
 inline int cuda_rc(int e) { return e == 0 ? SPECA_OK : SPECA_ERR_CUDA; }
 
@@ -398,6 +435,106 @@ int speca_commit_verify_tree(const speca_dims *dims, float *S, const uint16_t *k
     rc = cuda_rc(launch_pending_check(p, 8, st));
     if (rc != SPECA_OK) return rc;
     return cuda_rc(launch_verify_factorized(p, dims->d_k, true, false, st));
+}
+
+int speca_norm_rope(const speca_attn_dims *dims, const uint16_t *q, int64_t q_layer_stride, int64_t q_token_stride,
+                    const uint16_t *k, int64_t k_layer_stride, int64_t k_token_stride, const float *q_weight_or_null,
+                    const float *k_weight_or_null, float eps, const float *inv_freq, int32_t rot_dim, int32_t interleaved,
+                    float rope_scale, const int32_t *node_offsets, int32_t total_nodes, const int32_t *parent_or_null,
+                    const int32_t *kv_len, uint16_t *q_out, uint16_t *k_out, int32_t *status_word, void *stream)
+{
+    int rc = check_attn_dims(dims);
+    if (rc != SPECA_OK) return rc;
+    // (packed arrays of no nodes have no address)
+    if (!node_offsets || !kv_len || !status_word || (rot_dim > 0 && !inv_freq)) return SPECA_ERR_NULL;
+    if (total_nodes > 0 && (!q || !k || !q_out || !k_out)) return SPECA_ERR_NULL;
+    rc = check_attn_draft(dims, total_nodes, parent_or_null);
+    if (rc != SPECA_OK) return rc;
+    if (rot_dim < 0 || rot_dim > dims->d_head || rot_dim % 16 != 0) return SPECA_ERR_UNSUPPORTED;
+    if (!(eps >= 0.f)) return SPECA_ERR_RANGE;
+    // (a stride between things of which there is one is not looked at)
+    const bool layers = dims->n_layers > 1, tokens = total_nodes > 1;
+    if (tokens && (q_token_stride < 1LL * dims->heads * dims->d_head || k_token_stride < 1LL * dims->kv_heads * dims->d_head))
+        return SPECA_ERR_RANGE;
+    if (layers && (q_layer_stride < 0 || k_layer_stride < 0)) return SPECA_ERR_RANGE;
+    if (misaligned(q) || misaligned(k) || misaligned(q_out) || misaligned(k_out) || (q_weight_or_null && misaligned(q_weight_or_null)) ||
+        (k_weight_or_null && misaligned(k_weight_or_null)) || (tokens && (q_token_stride % 8 != 0 || k_token_stride % 8 != 0)) ||
+        (layers && (q_layer_stride % 8 != 0 || k_layer_stride % 8 != 0)))
+        return SPECA_ERR_ALIGN;
+    if (total_nodes == 0) return SPECA_OK;
+    AttnParams p = attn_params(dims, total_nodes);
+    p.q = bf(q); p.k = bf(k); p.node_offsets = node_offsets; p.parent = parent_or_null; p.kv_len = kv_len; p.status = status_word;
+    NormParams n{};
+    n.q_layer = layers ? q_layer_stride : 0; n.q_token = tokens ? q_token_stride : 0;
+    n.k_layer = layers ? k_layer_stride : 0; n.k_token = tokens ? k_token_stride : 0;
+    n.q_weight = q_weight_or_null; n.k_weight = k_weight_or_null; n.inv_freq = inv_freq;
+    n.q_out = bf(q_out); n.k_out = bf(k_out);
+    n.eps = eps; n.rope_scale = rope_scale; n.rot = rot_dim; n.interleaved = interleaved != 0;
+    return cuda_rc(launch_norm_rope(p, n, dims->d_head, static_cast<cudaStream_t>(stream)));
+}
+
+size_t speca_attn_workspace_bytes(const speca_attn_dims *dims)
+{
+    return check_attn_dims(dims) == SPECA_OK ? attend_workspace_bytes(dims) : 0;
+}
+
+int speca_attend_tree(const speca_attn_dims *dims, const uint16_t *q, const uint16_t *k, const uint16_t *v,
+                      const int32_t *node_offsets, int32_t total_nodes, const int32_t *parent_or_null,
+                      const uint16_t *k_cache, const uint16_t *v_cache, const int32_t *page_table, const int32_t *kv_len,
+                      uint16_t *o, void *workspace, size_t workspace_bytes, int32_t *status_word, void *stream)
+{
+    int rc = check_attn_dims(dims);
+    if (rc != SPECA_OK) return rc;
+    if (!node_offsets || !k_cache || !v_cache || !page_table || !kv_len || !status_word) return SPECA_ERR_NULL;
+    if (total_nodes > 0 && (!q || !k || !v || !o)) return SPECA_ERR_NULL;
+    if (!(dims->scale > 0.f) || !(dims->scale < 3.4e38f)) return SPECA_ERR_RANGE;
+    rc = check_attn_draft(dims, total_nodes, parent_or_null);
+    if (rc != SPECA_OK) return rc;
+    if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(k_cache) || misaligned(v_cache) || misaligned(o)) return SPECA_ERR_ALIGN;
+    if (!workspace || misaligned(workspace) || workspace_bytes < attend_workspace_bytes(dims)) return SPECA_ERR_WORKSPACE;
+    if (total_nodes == 0) return SPECA_OK;
+    AttnParams p = attn_params(dims, total_nodes);
+    p.q = bf(q); p.k = bf(k); p.v = bf(v); p.k_cache = bf(const_cast<uint16_t *>(k_cache)); p.v_cache = bf(const_cast<uint16_t *>(v_cache));
+    p.node_offsets = node_offsets; p.parent = parent_or_null; p.page_table = page_table; p.kv_len = kv_len; p.o = bf(o);
+    p.status = status_word; p.workspace = workspace;
+    return cuda_rc(launch_attend(p, dims->d_head, static_cast<cudaStream_t>(stream)));
+}
+
+int speca_commit_kv(const speca_attn_dims *dims, uint16_t *k_cache, uint16_t *v_cache, const int32_t *page_table,
+                    const int32_t *kv_len, const uint16_t *k, const uint16_t *v, const int32_t *node_offsets,
+                    int32_t total_nodes, const int32_t *parent_or_null, int32_t max_depth, const int32_t *path_idx_or_null,
+                    const int32_t *path_len_or_null, int32_t *kv_len_out, int32_t *status_word, void *stream)
+{
+    int rc = check_attn_dims(dims);
+    if (rc != SPECA_OK) return rc;
+    if (!k_cache || !v_cache || !page_table || !kv_len || !node_offsets || !kv_len_out || !status_word) return SPECA_ERR_NULL;
+    if (total_nodes > 0 && (!k || !v)) return SPECA_ERR_NULL;
+    if ((path_idx_or_null == nullptr) != (path_len_or_null == nullptr)) return SPECA_ERR_NULL;
+    const bool path = path_idx_or_null != nullptr;
+    rc = check_attn_draft(dims, total_nodes, path ? parent_or_null : nullptr);
+    if (rc != SPECA_OK) return rc;
+    if (path && (max_depth < 1 || max_depth > 16)) return SPECA_ERR_RANGE;
+    if (misaligned(k_cache) || misaligned(v_cache) || misaligned(k) || misaligned(v)) return SPECA_ERR_ALIGN;
+    AttnParams p = attn_params(dims, total_nodes);
+    p.k = bf(k); p.v = bf(v); p.k_cache = bf(k_cache); p.v_cache = bf(v_cache);
+    p.node_offsets = node_offsets; p.parent = path ? parent_or_null : nullptr; p.page_table = page_table; p.kv_len = kv_len;
+    p.path_idx = path_idx_or_null; p.path_len = path_len_or_null; p.max_depth = path ? max_depth : 0;
+    p.status = status_word;
+    return cuda_rc(launch_commit_kv(p, dims->d_head, kv_len_out, static_cast<cudaStream_t>(stream)));
+}
+
+int speca_copy_pages(const speca_attn_dims *dims, uint16_t *k_cache, uint16_t *v_cache, const int32_t *src, const int32_t *dst,
+                     int32_t n_copies, int32_t *status_word, void *stream)
+{
+    int rc = check_attn_dims(dims);
+    if (rc != SPECA_OK) return rc;
+    if (!k_cache || !v_cache || !status_word || (n_copies > 0 && (!src || !dst))) return SPECA_ERR_NULL;
+    if (n_copies < 0 || n_copies > dims->n_pages) return SPECA_ERR_RANGE;      // (more destinations than pages repeat one)
+    if (misaligned(k_cache) || misaligned(v_cache)) return SPECA_ERR_ALIGN;
+    if (n_copies == 0) return SPECA_OK;
+    AttnParams p = attn_params(dims, 0);
+    p.k_cache = bf(k_cache); p.v_cache = bf(v_cache); p.status = status_word;
+    return cuda_rc(launch_copy_pages(p, dims->d_head, src, dst, n_copies, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -33,18 +33,25 @@ struct Api {
     decltype(&speca_tree_mask_to_parent) tree_mask_to_parent;
     decltype(&speca_prune_tree) prune_tree;
     decltype(&speca_chain_decompose) chain_decompose;
+    decltype(&speca_norm_rope) norm_rope;
+    decltype(&speca_attend_tree) attend_tree;
+    decltype(&speca_commit_kv) commit_kv;
+    decltype(&speca_copy_pages) copy_pages;
 } g_api = {};
 
-enum Name { kLayers, kBatch, kHeads, kDk, kDv, kScale, kMaxDepth, kMaxNodes, kRoute, kRule, kK, kV, kAlpha, kBeta, kU, kOffsets, kTotal, kParent, kNames };
+enum Name { kLayers, kBatch, kHeads, kDk, kDv, kScale, kMaxDepth, kMaxNodes, kRoute, kRule, kK, kV, kAlpha, kBeta, kU, kOffsets, kTotal, kParent,
+            kKvHeads, kDHead, kPageSize, kNPages, kMaxPages, kNames };
 PyObject *g_name[kNames];
 const char *const kNameText[kNames] = {"n_layers", "batch", "heads", "d_k", "d_v", "scale", "max_depth", "max_nodes", "route", "rule",
-                                       "k", "v", "alpha", "beta", "u", "node_offsets", "total_nodes", "parent"};
+                                       "k", "v", "alpha", "beta", "u", "node_offsets", "total_nodes", "parent",
+                                       "kv_heads", "d_head", "page_size", "n_pages", "max_pages"};
 
 // Reads the arguments of one call; `ok` turns false at the first that is not plainly right.
 struct Reader {
     bool ok;
+    int device = -1;             // where every tensor has to be; -1: not looked at
 
-    Reader(Py_ssize_t n, Py_ssize_t want) : ok(n == want) {}
+    Reader(Py_ssize_t n, Py_ssize_t want, int on = -1) : ok(n == want), device(on) {}
 
     int integer(PyObject *o)
     {
@@ -76,11 +83,31 @@ struct Reader {
         if (PyErr_Occurred()) { PyErr_Clear(); ok = false; }
         return d;
     }
+    speca_attn_dims attn_dims(PyObject *o)
+    {
+        speca_attn_dims d;
+        d.n_layers = attr(o, kLayers); d.batch = attr(o, kBatch); d.heads = attr(o, kHeads); d.kv_heads = attr(o, kKvHeads);
+        d.d_head = attr(o, kDHead); d.max_nodes = attr(o, kMaxNodes); d.page_size = attr(o, kPageSize);
+        d.n_pages = attr(o, kNPages); d.max_pages = attr(o, kMaxPages);
+        PyObject *s = PyObject_GetAttr(o, g_name[kScale]);
+        d.scale = s != nullptr ? float(PyFloat_AsDouble(s)) : 0.f;
+        Py_XDECREF(s);
+        if (PyErr_Occurred()) { PyErr_Clear(); ok = false; }
+        return d;
+    }
+    float real(PyObject *o)
+    {
+        if (!ok || o == nullptr || !(PyFloat_Check(o) || PyLong_Check(o))) { ok = false; return 0.f; }
+        const float v = float(PyFloat_AsDouble(o));
+        if (PyErr_Occurred()) { PyErr_Clear(); ok = false; }       // an integer beyond every double
+        return v;
+    }
     const at::Tensor *tensor(PyObject *o, ScalarType type)
     {
         if (!ok || o == nullptr || !THPVariable_Check(o)) { ok = false; return nullptr; }
         const at::Tensor &t = THPVariable_Unpack(o);
         if (!t.is_cuda() || t.scalar_type() != type || !t.is_contiguous()) { ok = false; return nullptr; }
+        if (device >= 0 && t.get_device() != device) { ok = false; return nullptr; }
         return &t;
     }
     // device pointer of a tensor of this type and shape; None is a null pointer
@@ -357,6 +384,102 @@ PyObject *chain_decompose(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// heads [L][T][H][d] of rows that may be wider: dense in a token, strides between layers and tokens as they come
+struct Heads {
+    uint16_t *ptr = nullptr;
+    int64_t layer = 0, token = 0;
+    Heads(Reader &r, PyObject *o, int64_t L, int64_t T, int64_t H, int64_t D)
+    {
+        if (!r.ok || !THPVariable_Check(o)) { r.ok = false; return; }
+        const at::Tensor &t = THPVariable_Unpack(o);
+        if (!t.is_cuda() || t.scalar_type() != ScalarType::BFloat16 || !(t.sizes() == at::IntArrayRef({L, T, H, D})) ||
+            t.get_device() != r.device || t.stride(3) != 1 || (H > 1 && t.stride(2) != D)) { r.ok = false; return; }
+        ptr = static_cast<uint16_t *>(t.data_ptr());
+        layer = t.stride(0);
+        token = t.stride(1);
+    }
+};
+
+PyObject *norm_rope(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Reader r(n, 17, c10::cuda::current_device());
+    if (!r.ok) Py_RETURN_NONE;
+    const speca_attn_dims d = r.attn_dims(a[0]);
+    const int64_t L = d.n_layers, B = d.batch, H = d.heads, K = d.kv_heads, D = d.d_head;
+    const int rot = r.integer(a[7]), T = r.integer(a[11]);
+    const float eps = r.real(a[5]), scale = r.real(a[9]);
+    const int inter = PyObject_IsTrue(a[8]);
+    if (inter < 0) { PyErr_Clear(); Py_RETURN_NONE; }
+    const Heads q(r, a[1], L, T, H, D), k(r, a[2], L, T, K, D);
+    float *wq = r.f32(a[3], {L, D}), *wk = r.f32(a[4], {L, D}), *freq = r.f32(a[6], {rot / 2});
+    int32_t *offs = r.i32(a[10], {B + 1}), *par = r.i32(a[12], {T}), *len = r.i32(a[13], {B});
+    uint16_t *qo = r.bf16(a[14], {L, T, H, D}), *ko = r.bf16(a[15], {L, T, K, D});
+    int32_t *status = r.i32(a[16], {1});
+    return call(r, [&](void *st) {
+        return g_api.norm_rope(&d, q.ptr, q.layer, q.token, k.ptr, k.layer, k.token, wq, wk, eps, freq, rot, inter, scale, offs, T,
+                               par, len, qo, ko, status, st);
+    });
+}
+
+PyObject *attend_tree(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Reader r(n, 14, c10::cuda::current_device());
+    if (!r.ok) Py_RETURN_NONE;
+    const speca_attn_dims d = r.attn_dims(a[0]);
+    const int64_t L = d.n_layers, B = d.batch, H = d.heads, K = d.kv_heads, D = d.d_head;
+    const int T = r.integer(a[5]);
+    uint16_t *q = r.bf16(a[1], {L, T, H, D}), *k = r.bf16(a[2], {L, T, K, D}), *v = r.bf16(a[3], {L, T, K, D});
+    int32_t *offs = r.i32(a[4], {B + 1}), *par = r.i32(a[6], {T});
+    uint16_t *kc = r.bf16(a[7], {L, d.n_pages, K, d.page_size, D}), *vc = r.bf16(a[8], {L, d.n_pages, K, d.page_size, D});
+    int32_t *table = r.i32(a[9], {B, d.max_pages}), *len = r.i32(a[10], {B});
+    uint16_t *o = r.bf16(a[11], {L, T, H, D});
+    const Reader::Bytes ws = r.bytes(a[12]);
+    int32_t *status = r.i32(a[13], {1});
+    return call(r, [&](void *st) {
+        return g_api.attend_tree(&d, q, k, v, offs, T, par, kc, vc, table, len, o, ws.ptr, ws.size, status, st);
+    });
+}
+
+PyObject *commit_kv(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Reader r(n, 14, c10::cuda::current_device());
+    if (!r.ok) Py_RETURN_NONE;
+    const speca_attn_dims d = r.attn_dims(a[0]);
+    const int64_t L = d.n_layers, B = d.batch, K = d.kv_heads, D = d.d_head;
+    const int T = r.integer(a[8]);
+    uint16_t *kc = r.bf16(a[1], {L, d.n_pages, K, d.page_size, D}), *vc = r.bf16(a[2], {L, d.n_pages, K, d.page_size, D});
+    int32_t *table = r.i32(a[3], {B, d.max_pages}), *len = r.i32(a[4], {B});
+    uint16_t *k = r.bf16(a[5], {L, T, K, D}), *v = r.bf16(a[6], {L, T, K, D});
+    int32_t *offs = r.i32(a[7], {B + 1}), *par = r.i32(a[9], {T});
+    int64_t depth = 0;
+    int32_t *idx = nullptr, *plen = r.i32(a[11], {B});
+    if (a[10] != Py_None) {
+        const at::Tensor *t = r.any(a[10], ScalarType::Int, 2);
+        if (!r.ok || t->size(0) != B || t->size(1) > INT32_MAX) Py_RETURN_NONE;
+        depth = t->size(1);
+        idx = static_cast<int32_t *>(t->data_ptr());
+    }
+    int32_t *out = r.i32(a[12], {B}), *status = r.i32(a[13], {1});
+    return call(r, [&](void *st) {
+        return g_api.commit_kv(&d, kc, vc, table, len, k, v, offs, T, par, int(depth), idx, plen, out, status, st);
+    });
+}
+
+PyObject *copy_pages(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Reader r(n, 6, c10::cuda::current_device());
+    if (!r.ok) Py_RETURN_NONE;
+    const speca_attn_dims d = r.attn_dims(a[0]);
+    const int64_t L = d.n_layers, K = d.kv_heads, D = d.d_head;
+    uint16_t *kc = r.bf16(a[1], {L, d.n_pages, K, d.page_size, D}), *vc = r.bf16(a[2], {L, d.n_pages, K, d.page_size, D});
+    const at::Tensor *src = r.any(a[3], ScalarType::Int, 1);
+    if (!r.ok || src->numel() > INT32_MAX) Py_RETURN_NONE;
+    const int64_t count = src->numel();
+    const int32_t *from = src->const_data_ptr<int32_t>();
+    int32_t *to = r.i32(a[4], {count}), *status = r.i32(a[5], {1});
+    return call(r, [&](void *st) { return g_api.copy_pages(&d, kc, vc, from, to, int(count), status, st); });
+}
+
 // bind({entry point name without "speca_": address})
 PyObject *bind(PyObject *, PyObject *table)
 {
@@ -379,6 +502,10 @@ PyObject *bind(PyObject *, PyObject *table)
     get("tree_mask_to_parent", g_api.tree_mask_to_parent);
     get("prune_tree", g_api.prune_tree);
     get("chain_decompose", g_api.chain_decompose);
+    get("norm_rope", g_api.norm_rope);
+    get("attend_tree", g_api.attend_tree);
+    get("commit_kv", g_api.commit_kv);
+    get("copy_pages", g_api.copy_pages);
     if (!ok) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "bind: an entry point is missing");
         return nullptr;
@@ -401,7 +528,8 @@ PyObject *guarded(PyObject *self, PyObject *const *a, Py_ssize_t n)
 PyMethodDef kMethods[] = {
     FAST(decode_step), FAST(verify_chain), FAST(verify_tree), FAST(verify_tree_noalloc), FAST(greedy_accept),
     FAST(stochastic_accept), FAST(commit), FAST(commit_verify_tree), FAST(commit_conv), FAST(tree_mask_to_parent),
-    FAST(prune_tree), FAST(chain_decompose), {"bind", bind, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+    FAST(prune_tree), FAST(chain_decompose), FAST(norm_rope), FAST(attend_tree), FAST(commit_kv), FAST(copy_pages),
+    {"bind", bind, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "speca_marshal", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
