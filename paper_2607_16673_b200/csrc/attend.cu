@@ -1,85 +1,857 @@
 // Verification by an attention layer: draft nodes attend the committed rows of a paged cache and their own ancestors.
+//
+// For a key head the rows of a product are the (node, query head) pairs of a sequence that share it, up to 128 a tile; the
+// columns are keys.  Per tile of N keys:  S = Q K^T (both operands in shared memory, K as its pages lie), the weights
+// P = exp2((S - m) scale log2 e) with a running maximum m, rounded to bf16 and written over S in TMEM, and O += P V with P
+// from TMEM and V as its pages lie (keys along the rows: an MN-major operand).  O stays in TMEM; it is scaled down only when
+// a row's maximum has grown by more than kSlack, so that a weight is at most 2^kSlack and the sum of weights, kept in fp32,
+// and O are in the same scale whatever that scale is.
+//
+// Work: the tiles of all (sequence, layer, key head, row tile) units stand in one list, and every CTA takes an equal piece of
+// it, so the batch's lengths do not matter and a single long context occupies every SM.  A unit cut by the border of two
+// pieces leaves unnormalised sums with their maxima in the workspace, which a second kernel joins in the order of the pieces.
 #include "attn.cuh"
+#include "tc_ptx.cuh"
 
 namespace speca {
+
+using namespace tc;
+
 namespace {
 
-constexpr int kWarps = 4;
+constexpr int kMaxCtas = 160;            // pieces of the list at most (148 SMs)
+constexpr int kRecords = 4;              // ring of segment records
+constexpr float kSlack = 8.f;            // binary digits a maximum may grow by before O is scaled
+constexpr int kFlagRing = 8;
 
-// One warp a row (node, query head): keys one at a time, running maximum and sum.
+// D <= 128: two softmax groups of 128 rows, each with an O of its own.  A unit of at most 128 rows has its even key tiles in
+// one and the odd ones in the other, joined at the end; a larger one has a row tile in each, over the same keys.  D = 256: O
+// alone takes half of TMEM; one group, and S of the next tile is formed while it works on this one.
+template <int D> struct Cfg {
+    static constexpr int N = D == 256 ? 64 : 128;
+    static constexpr int LANES = D == 256 ? 1 : 2;
+    static constexpr int MT = 128 * LANES;
+    static constexpr int SOFT = 4 * LANES;                   // softmax warps; then TMA, MMA, mending of V, schedule
+    static constexpr int THREADS = (SOFT + 4) * 32;
+    static constexpr int Q_BYTES = 128 * D * 2;
+    static constexpr int TILE = N * D * 2;                   // keys or values of a tile
+    static constexpr int SLOTS = D == 64 ? 10 : 5;
+    static constexpr int OffQ = 0;
+    static constexpr int OffRing = LANES * Q_BYTES;
+    static constexpr int OffPar = OffRing + SLOTS * TILE;    // int16 parent[kAttnMaxTree]; scratch of the scan before that
+    static constexpr int OffRec = OffPar + 2 * kAttnMaxTree;
+    static constexpr int OffBars = OffRec + 64 * kRecords;
+    static constexpr int kFull = 0, kEmpty = SLOTS, kRaw = 2 * SLOTS, kSFull = 3 * SLOTS, kPReady = kSFull + 2, kODone = kPReady + 2,
+                         kQFull = kODone + 2, kSync = kQFull + 1, kRecFull = kSync + 1, kRecEmpty = kRecFull + kRecords,
+                         kDrain = kRecEmpty + kRecords, kBars = kDrain + 1;
+    static constexpr int OffMisc = OffBars + 8 * kBars;      // abort, TMEM base, bad topology [2], start of the piece [4]
+    static constexpr int OffFlags = OffMisc + 64;            // segment numbers: bad page [8], values that are not finite [8]
+    static constexpr int Bytes = OffFlags + 8 * kFlagRing;
+};
+static_assert(Cfg<128>::Bytes <= 232448 && Cfg<256>::Bytes <= 232448 && Cfg<64>::Bytes <= 232448, "shared memory of a CTA");
+
+constexpr int kTmemCols = 512, kOCol = 256;                  // S (P) buffers at 0 and N, O from column 256
+
+// A piece of one unit: key tiles t0 .. t1-1, of which the first `ct` of the unit are the cache's.
+struct Rec {
+    int l, b, hk, base;
+    int n, len, row0, rows;
+    int t0, t1, ct, nodes;                                   // nodes: draft nodes the unit's rows can see (0 .. nodes-1)
+    int slot, index, pad0, pad1;                             // slot: -1 the whole unit, 0 / 1 where its sums go
+};
+static_assert(sizeof(Rec) == 64, "record");
+
+// Joining: what a CTA's unit that goes on in the next CTAs needs.
+struct Join {
+    int parts, l, hk, base;
+    int row0, rows, pad0, pad1;
+};
+
+struct Plan {
+    int rows_cap;                                            // rows of a slot
+    size_t slot_bytes;
+    Join *join;
+    char *slots;
+};
+
+__host__ __device__ inline size_t slot_bytes(int rows, int d) { return align256(size_t(rows) * d * 4 + size_t(rows) * 8 + 16); }
+inline int slot_rows(int max_nodes, int group, int mt) { return int(1LL * max_nodes * group < mt ? 1LL * max_nodes * group : mt); }
+
+__device__ __forceinline__ float *slot_sums(const Plan &pl, int cta, int slot)
+{
+    return reinterpret_cast<float *>(pl.slots + (size_t(cta) * 2 + slot) * pl.slot_bytes);
+}
+
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float *r)
+{
+    uint32_t x[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
+        "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7]), "=r"(x[8]), "=r"(x[9]),
+          "=r"(x[10]), "=r"(x[11]), "=r"(x[12]), "=r"(x[13]), "=r"(x[14]), "=r"(x[15]), "=r"(x[16]), "=r"(x[17]), "=r"(x[18]),
+          "=r"(x[19]), "=r"(x[20]), "=r"(x[21]), "=r"(x[22]), "=r"(x[23]), "=r"(x[24]), "=r"(x[25]), "=r"(x[26]), "=r"(x[27]),
+          "=r"(x[28]), "=r"(x[29]), "=r"(x[30]), "=r"(x[31])
+        : "r"(taddr)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) r[i] = __uint_as_float(x[i]);
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&x)[16])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+        ::"r"(taddr), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]), "r"(x[8]),
+          "r"(x[9]), "r"(x[10]), "r"(x[11]), "r"(x[12]), "r"(x[13]), "r"(x[14]), "r"(x[15])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// kind::f16 (bf16) with the A operand in TMEM: a 32-bit column holds two consecutive K elements, the even one low
+__device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate,
+                                            uint32_t lead)
+{
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "setp.ne.b32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(lead)
+        : "memory");
+}
+// MN-major operand (rows are K, 128 bytes of MN a row), 128-byte swizzle: `block` bytes from one 64-wide block of MN to the
+// next, 1024 from one group of eight rows to the next
+__device__ __forceinline__ uint64_t make_desc_mn(uint32_t smem_addr, uint32_t block)
+{
+    uint64_t d = 0;
+    d |= uint64_t((smem_addr >> 4) & 0x3fffu);
+    d |= uint64_t((block >> 4) & 0x3fffu) << 16;
+    d |= uint64_t(1024 >> 4) << 32;
+    d |= uint64_t(1) << 46;
+    d |= uint64_t(2) << 61;
+    return d;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ float exp2_approx(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ bool not_finite(uint32_t pair)
+{
+    return (pair & 0x7f80u) == 0x7f80u || (pair & 0x7f800000u) == 0x7f800000u;
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// The list of tiles
+// ---------------------------------------------------------------------------------------------------------------
+struct Seq {
+    int base, n, len, ct, fault;
+};
+
+template <int N> __device__ __forceinline__ Seq sequence(const AttnParams &p, int b)
+{
+    Seq s;
+    s.fault = sequence_nodes(p, b, s.base, s.n);
+    s.len = p.kv_len[b];
+    if (s.len < 0 || (s.len >> p.page_shift) > p.max_pages || s.len > p.max_pages << p.page_shift) s.fault |= SPECA_STATUS_BAD_PAGE;
+    if (s.fault) s.n = 0;
+    s.ct = s.fault ? 0 : (s.len + N - 1) / N;
+    return s;
+}
+// draft nodes that the rows of row tile m can see
+template <int MT> __device__ __forceinline__ int nodes_seen(int n, int group, int m)
+{
+    return min(n, ((m + 1) * MT - 1) / group + 1);
+}
+template <int D> __device__ __forceinline__ long unit_tiles(const Seq &s, int group, int m)
+{
+    return s.ct + (nodes_seen<Cfg<D>::MT>(s.n, group, m) + Cfg<D>::N - 1) / Cfg<D>::N;
+}
+template <int D> __device__ __forceinline__ int row_tiles(const Seq &s, int group)
+{
+    return (s.n * group + Cfg<D>::MT - 1) / Cfg<D>::MT;     // (at most 8192 nodes and 65536 heads)
+}
+// tiles of one layer and key head
+template <int D> __device__ __forceinline__ long head_tiles(const Seq &s, int group)
+{
+    long sum = 0;
+    for (int m = 0; m < row_tiles<D>(s, group); ++m) sum += unit_tiles<D>(s, group, m);
+    return sum;
+}
+
 template <int D>
-__global__ void __launch_bounds__(kWarps * 32)
-attend_kernel(AttnParams p)
+__global__ void __launch_bounds__(Cfg<D>::THREADS, 1)
+attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
+              const __grid_constant__ CUtensorMap kd_map, const __grid_constant__ CUtensorMap vd_map, AttnParams p, Plan plan,
+              int32_t box_rows)
 {
     after_previous_kernel();
-    constexpr int E = D / 32;
-    const int lane = threadIdx.x & 31;
-    const long task = long(blockIdx.x) * kWarps + (threadIdx.x >> 5);
-    if (task >= long(p.L) * p.T * p.H) return;
-    const int h = int(task % p.H), t = int(task / p.H % p.T), l = int(task / p.H / p.T), hk = h / (p.H / p.HK);
-    int b = 0;
-    for (int i = lane; i < p.B; i += 32) b += p.node_offsets[i + 1] <= t;
-    b = __reduce_add_sync(0xffffffffu, b);
-    int base = 0, n = 0, fault = b >= p.B ? SPECA_STATUS_BAD_OFFSETS : sequence_nodes(p, b, base, n);
-    if (!fault && t < base) fault = SPECA_STATUS_BAD_OFFSETS;
-    const int page = 1 << p.page_shift;
-    const int32_t *table = nullptr;
-    int len = 0;
-    if (!fault) {
-        table = p.page_table + size_t(b) * p.max_pages;
-        len = p.kv_len[b];
-        int bad = len < 0 || len > (p.max_pages << p.page_shift);
-        if (!bad)
-            for (int i = lane; i < (len + page - 1) >> p.page_shift; i += 32) bad |= table[i] < 0 || table[i] >= p.n_pages;
-        if (__any_sync(0xffffffffu, bad)) fault |= SPECA_STATUS_BAD_PAGE;
-        bad = 0;
-        if (p.parent != nullptr)
-            for (int i = lane; i < n; i += 32) bad |= p.parent[base + i] < -1 || p.parent[base + i] >= i;
-        if (__any_sync(0xffffffffu, bad)) fault |= SPECA_STATUS_BAD_PARENT;
-    }
-    if (fault) {
-        if (lane == 0 && l == 0 && h == 0) atomicOr(p.status, fault);
+    using C = Cfg<D>;
+    constexpr int N = C::N, LANES = C::LANES, SOFT = C::SOFT, SLOTS = C::SLOTS;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const uint32_t sbase = smem_u32(smem);
+    if (sbase & 1023u) {                                     // never expected; refuse to run rather than corrupt
+        if (threadIdx.x == 0) atomicOr(p.status, SPECA_STATUS_TIMEOUT);
         return;
     }
-    float q[E], o[E], m = -INFINITY, sum = 0.f;
-    const size_t row = (size_t(l) * p.T + t) * p.H + h;
-    for (int i = 0; i < E; ++i) { q[i] = __bfloat162float(p.q[row * D + lane + 32 * i]) * p.scale; o[i] = 0.f; }
-    auto take = [&](const __nv_bfloat16 *k, const __nv_bfloat16 *v) {
-        float s = 0.f;
-        for (int i = 0; i < E; ++i) s = fmaf(q[i], __bfloat162float(k[lane + 32 * i]), s);
-        for (int w = 16; w > 0; w /= 2) s += __shfl_xor_sync(0xffffffffu, s, w);
-        const float top = fmaxf(m, s), old = m == top ? 1.f : expf(m - top), e = expf(s - top);
-        sum = sum * old + e;
-        for (int i = 0; i < E; ++i) o[i] = o[i] * old + e * __bfloat162float(v[lane + 32 * i]);
-        m = top;
+    auto bar = [&](int i) { return sbase + C::OffBars + 8u * uint32_t(i); };
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + C::OffMisc);
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + C::OffMisc + 4);
+    volatile int *topo_bad = reinterpret_cast<volatile int *>(smem + C::OffMisc + 8);      // [2]
+    volatile int *start = reinterpret_cast<volatile int *>(smem + C::OffMisc + 16);        // sequence, then tiles into it (64 bits)
+    volatile int *page_bad = reinterpret_cast<volatile int *>(smem + C::OffFlags);         // [kFlagRing] 1 + segment number
+    volatile int *value_bad = page_bad + kFlagRing;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int group = p.H / p.HK;
+    const int grid = gridDim.x, cta = blockIdx.x;
+
+    if (threadIdx.x == 0) {
+        *abort_flag = 0;
+        topo_bad[0] = topo_bad[1] = 0;
+        for (int i = 0; i < 2 * kFlagRing; ++i) page_bad[i] = 0;
+        for (int i = 0; i < SLOTS; ++i) { mbar_init(bar(C::kFull + i), 1); mbar_init(bar(C::kEmpty + i), 1); mbar_init(bar(C::kRaw + i), 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(bar(C::kSFull + i), 1); mbar_init(bar(C::kPReady + i), 4); mbar_init(bar(C::kODone + i), 1); }
+        mbar_init(bar(C::kQFull), SOFT);
+        mbar_init(bar(C::kSync), SOFT);
+        for (int i = 0; i < kRecords; ++i) { mbar_init(bar(C::kRecFull + i), 1); mbar_init(bar(C::kRecEmpty + i), SOFT + 3); }
+        mbar_init(bar(C::kDrain), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == SOFT + 1) tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_slot)), kTmemCols);
+
+    // ---- tiles of the whole list, and where this CTA's piece begins: every thread has some consecutive sequences
+    long mine = 0, before = 0, total = 0;
+    const int per_thread = (p.B + C::THREADS - 1) / C::THREADS;
+    const int b_lo = min(p.B, int(threadIdx.x) * per_thread), b_hi = min(p.B, b_lo + per_thread);
+    const long heads = long(p.L) * p.HK;
+    for (int b = b_lo; b < b_hi; ++b) {
+        const Seq s = sequence<N>(p, b);
+        if (s.fault && cta == 0) atomicOr(p.status, s.fault);
+        mine += heads * head_tiles<D>(s, group);
+    }
+    long incl = mine;
+#pragma unroll
+    for (int i = 1; i < 32; i *= 2) {
+        const long x = __shfl_up_sync(0xffffffffu, incl, i);
+        if (lane >= i) incl += x;
+    }
+    volatile long *sums = reinterpret_cast<volatile long *>(smem + C::OffPar);
+    if (lane == 31) sums[warp] = incl;
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    for (int w = 0; w < C::THREADS / 32; ++w) {
+        if (w < warp) before += sums[w];
+        total += sums[w];
+    }
+    before += incl - mine;
+    const long per = total / grid, extra = total % grid;
+    const long begin = cta * per + min(long(cta), extra), count = per + (cta < extra ? 1 : 0);
+    if (count > 0 && begin >= before && begin < before + mine) {
+        long rem = begin - before;
+        int b = b_lo;
+        for (;; ++b) {
+            const long t = heads * head_tiles<D>(sequence<N>(p, b), group);
+            if (rem < t) break;
+            rem -= t;
+        }
+        start[0] = b;
+        start[2] = int(rem & 0xffffffffL);
+        start[3] = int(rem >> 32);
+    }
+    __syncthreads();
+    const uint32_t tmem = *tmem_slot;
+    const uint32_t lead = elect_one();
+    bool ok = true;
+
+    // record of segment `s`; false: the list has ended, or (ok == false) the CTA is aborting
+    auto record = [&](uint32_t s, Rec &r) -> bool {
+        if (!(ok = wait_fast(bar(C::kRecFull + (s % kRecords)), (s / kRecords) & 1, abort_flag))) return false;
+        const int4 *src = reinterpret_cast<const int4 *>(smem + C::OffRec) + 4 * (s % kRecords);
+        const int4 a = src[0], b = src[1], c = src[2], d = src[3];
+        r = Rec{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w, c.x, c.y, c.z, c.w, d.x, d.y, 0, 0};
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::kRecEmpty + (s % kRecords)));
+        return r.rows > 0;
     };
-    for (int j = 0; j < len; ++j) {
-        const size_t at = (((size_t(l) * p.n_pages + table[j >> p.page_shift]) * p.HK + hk) << p.page_shift) + (j & (page - 1));
-        take(p.k_cache + at * D, p.v_cache + at * D);
+    // rows of tile t that hold keys
+    auto valid_of = [&](const Rec &r, int t) {
+        const int left = t < r.ct ? r.len - t * N : r.nodes - (t - r.ct) * N;
+        return left < N ? left : N;
+    };
+    // whose values are looked over before they are used: they land on a barrier of their own (the warp that does it skips the
+    // other tiles, so it could not tell two phases of the common barrier apart)
+    auto to_mend = [&](const Rec &r, int t) { return t >= r.ct || (valid_of(r, t) & 15) != 0; };
+    Rec r;
+
+    if (warp == SOFT) {
+        // ------------------------------------------------------------------------------- keys and values, by TMA
+        uint32_t it = 0;
+        for (uint32_t seg = 0; ok && record(seg, r); ++seg) {
+            const int32_t *table = p.page_table + size_t(r.b) * p.max_pages;
+            const int pages = (r.len + (1 << p.page_shift) - 1) >> p.page_shift;
+            int window = (r.t0 * N) >> p.page_shift;         // 32 entries of the table, one a lane, and the 32 behind them
+            auto entries = [&](int first) { return r.t0 < r.ct && first + lane < pages ? table[first + lane] : 0; };
+            int ids = entries(window), next = entries(window + 32);
+#pragma unroll 1
+            for (int t = r.t0; t < r.t1 && ok; ++t) {
+                const int valid = valid_of(r, t);
+                const bool draft = t >= r.ct;
+                const int rows = draft ? 16 : box_rows, boxes = (valid + rows - 1) / rows;
+                int y = 0, z = 0;                            // this lane's box: rows into its page, the page and head
+                if (draft) {
+                    y = r.hk;
+                    z = r.l * p.T + r.base + (t - r.ct) * N + lane * 16;
+                } else {
+                    const int at = t * N + lane * rows, page = at >> p.page_shift, first = (t * N) >> p.page_shift;
+                    if (first >= window + 32) {
+                        window = first;
+                        ids = next;
+                        next = entries(window + 32);
+                    }
+                    int id = __shfl_sync(0xffffffffu, ids, (page - window) & 31);
+                    if (lane < boxes && (id < 0 || id >= p.n_pages)) {
+                        id = 0;                              // read what is there, and leave the unit's outputs alone
+                        page_bad[seg % kFlagRing] = int(seg) + 1;
+                        atomicOr(p.status, SPECA_STATUS_BAD_PAGE);
+                    }
+                    y = at & ((1 << p.page_shift) - 1);
+                    z = (r.l * p.n_pages + id) * p.HK + r.hk;
+                }
+                __syncwarp();
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv, ++it) {
+                    const int s = it % SLOTS;
+                    if (!(ok = wait_fast(bar(C::kEmpty + s), ((it / SLOTS) & 1) ^ 1, abort_flag))) break;
+                    const uint32_t full = bar((kv == 1 && to_mend(r, t) ? C::kRaw : C::kFull) + s);
+                    if (lane == 0) mbar_arrive_expect_tx(full, uint32_t(boxes) * rows * (D * 2));
+                    __syncwarp();
+                    if (lane < boxes) {
+                        const CUtensorMap *map = draft ? (kv ? &vd_map : &kd_map) : (kv ? &v_map : &k_map);
+#pragma unroll
+                        for (int c = 0; c < D / 64; ++c)
+                            tma_load_3d(sbase + C::OffRing + s * C::TILE + c * (N * 128) + lane * rows * 128, map, c * 64, y, z, full);
+                    }
+                    __syncwarp();
+                }
+            }
+        }
+    } else if (warp == SOFT + 1) {
+        // ------------------------------------------------------------------------------- products
+        const uint32_t id_s = make_idesc_bf16(N), id_o = make_idesc_bf16(D) | (1u << 16);      // (B of the second is MN-major)
+        uint32_t tiles = 0, p_count[2] = {0, 0};
+        for (uint32_t seg = 0; ok && record(seg, r); ++seg) {
+            const bool two = LANES == 2 && r.rows > 128;     // two row tiles over the same keys
+            const int items = (r.t1 - r.t0) << (two ? 1 : 0);
+            if (!(ok = wait_fast(bar(C::kQFull), seg & 1, abort_flag))) break;
+            tc_fence_after();
+            auto scores = [&](int i) -> bool {
+                const uint32_t kt = 2 * (tiles + (two ? i >> 1 : i)), s = kt % SLOTS;
+                const int buf = i & 1;
+                if (!two || buf == 0) {
+                    if (!wait_fast(bar(C::kFull + s), (kt / SLOTS) & 1, abort_flag)) return false;
+                }
+                // the weights of two items ago, in the same columns, have been used
+                if (i >= 2 && !wait_fast(bar(C::kODone + buf), (p_count[buf] - 1) & 1, abort_flag)) return false;
+                tc_fence_after();
+                const uint32_t qa = sbase + C::OffQ + (two ? buf * C::Q_BYTES : 0), ka = sbase + C::OffRing + s * C::TILE;
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k)
+                    mma_bf16(tmem + buf * N, make_desc(qa + (k >> 2) * (128 * 128) + (k & 3) * 32),
+                             make_desc(ka + (k >> 2) * (N * 128) + (k & 3) * 32), id_s, k != 0, lead);
+                mma_commit(bar(C::kSFull + buf), lead);
+                if (!two || buf == 1) mma_commit(bar(C::kEmpty + s), lead);
+                return true;
+            };
+            if (!(ok = scores(0))) break;
+#pragma unroll 1
+            for (int i = 0; i < items && ok; ++i) {
+                if (i + 1 < items && !(ok = scores(i + 1))) break;
+                const int buf = i & 1, t = r.t0 + (two ? i >> 1 : i), valid = valid_of(r, t);
+                const uint32_t vt = 2 * (tiles + (two ? i >> 1 : i)) + 1, s = vt % SLOTS;
+                if ((!two || buf == 0) && !(ok = wait_fast(bar(C::kFull + s), (vt / SLOTS) & 1, abort_flag))) break;
+                if (!(ok = wait_fast(bar(C::kPReady + buf), p_count[buf] & 1, abort_flag))) break;
+                ++p_count[buf];
+                tc_fence_after();
+                const int oc = LANES == 2 ? kOCol + buf * D : kOCol, steps = (valid + 15) >> 4;
+                const bool fresh = LANES == 2 ? i < 2 : i == 0;
+                const uint64_t vd = make_desc_mn(sbase + C::OffRing + s * C::TILE, N * 128);
+#pragma unroll
+                for (int k = 0; k < N / 16; ++k)
+                    if (k < steps)
+                        mma_bf16_ts(tmem + oc, tmem + buf * N + 8 * k, vd + uint64_t(k * (16 * 128 >> 4)), id_o, !(fresh && k == 0), lead);
+                mma_commit(bar(C::kODone + buf), lead);
+                if (!two || buf == 1) mma_commit(bar(C::kEmpty + s), lead);
+            }
+            tiles += r.t1 - r.t0;
+        }
+    } else if (warp == SOFT + 2) {
+        // ------------------------------------------------------------------------------- mending of V
+        // A weight of zero does not take a value that is not finite out of a product: rows past the end of a tile's keys (what
+        // was there before, another sequence's, or never written) are set to zero, and so are draft values that are not finite,
+        // which only some rows attend; those get them back at the end.
+        uint32_t tiles = 0, phase = 0;                       // phase: a bit a slot
+        for (uint32_t seg = 0; ok && record(seg, r); ++seg) {
+#pragma unroll 1
+            for (int t = r.t0; t < r.t1; ++t, ++tiles) {
+                if (!to_mend(r, t)) continue;
+                const int valid = valid_of(r, t);
+                const bool draft = t >= r.ct;
+                const uint32_t s = (2 * tiles + 1) % SLOTS;
+                if (!(ok = wait_fast(bar(C::kRaw + s), (phase >> s) & 1, abort_flag))) break;
+                phase ^= 1u << s;
+                uint8_t *v = smem + C::OffRing + s * C::TILE;
+                const int end = (valid + 15) & ~15;
+                for (int i = valid * (D / 8) + lane; i < end * (D / 8); i += 32) {
+                    const int row = i / (D / 8), c = i % (D / 8);
+                    *reinterpret_cast<uint4 *>(v + (c >> 3) * (N * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+                }
+                if (draft) {
+                    bool bad = false;
+#pragma unroll 4
+                    for (int i = lane; i < valid * (D / 8); i += 32) {
+                        const int row = i / (D / 8), c = i % (D / 8);
+                        uint4 *at = reinterpret_cast<uint4 *>(v + (c >> 3) * (N * 128) + row * 128 + (c & 7) * 16);
+                        const uint4 x = *at;
+                        if (not_finite(x.x) || not_finite(x.y) || not_finite(x.z) || not_finite(x.w)) {
+                            uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                if ((w[e] & 0x7f80u) == 0x7f80u) w[e] &= 0xffff0000u;
+                                if ((w[e] & 0x7f800000u) == 0x7f800000u) w[e] &= 0xffffu;
+                            }
+                            *at = make_uint4(w[0], w[1], w[2], w[3]);
+                            bad = true;
+                        }
+                    }
+                    if (bad) value_bad[seg % kFlagRing] = int(seg) + 1;
+                }
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(C::kFull + s));
+            }
+        }
+    } else if (warp == SOFT + 3) {
+        // ------------------------------------------------------------------------------- schedule
+        Join join{0, 0, 0, 0, 0, 0, 0, 0};
+        uint32_t seg = 0;
+        auto put = [&](const Rec &x) {
+            ok = seg < kRecords || wait_fast(bar(C::kRecEmpty + (seg % kRecords)), ((seg / kRecords) & 1) ^ 1, abort_flag);
+            if (!ok) return;
+            if (lane == 0) {
+                *reinterpret_cast<Rec *>(smem + C::OffRec + 64 * (seg % kRecords)) = x;
+                mbar_arrive(bar(C::kRecFull + (seg % kRecords)));
+            }
+            __syncwarp();
+            ++seg;
+        };
+        long left = count;
+        if (left > 0) {
+            int b = start[0];
+            long rem = (long(start[3]) << 32) | uint32_t(start[2]);
+            long at = begin;                                 // place in the whole list
+            for (; left > 0 && ok; ++b, rem = 0) {
+                const Seq s = sequence<N>(p, b);
+                const long ht = head_tiles<D>(s, group);
+                if (ht == 0) continue;
+                long hd = rem / ht, in = rem % ht;
+                const int mts = row_tiles<D>(s, group);
+                for (; hd < heads && left > 0 && ok; ++hd, in = 0) {
+                    for (int m = 0; m < mts && left > 0 && ok; ++m) {
+                        const long ut = unit_tiles<D>(s, group, m);
+                        if (in >= ut) { in -= ut; continue; }
+                        const long take = min(left, ut - in);
+                        Rec x{};
+                        x.l = int(hd / p.HK); x.b = b; x.hk = int(hd % p.HK); x.base = s.base; x.n = s.n; x.len = s.len;
+                        x.row0 = m * C::MT;
+                        x.rows = int(min(long(C::MT), long(s.n) * group - x.row0));
+                        x.t0 = int(in); x.t1 = int(in + take); x.ct = s.ct;
+                        x.nodes = nodes_seen<C::MT>(s.n, group, m);
+                        x.slot = take == ut ? -1 : in == 0 ? 1 : 0;
+                        if (x.slot == 1) {
+                            // the unit ends in a later CTA's piece
+                            const long last = at + ut - 1, wide = extra * (per + 1);
+                            const int owner = int(last < wide ? last / (per + 1) : extra + (last - wide) / per);
+                            join = Join{owner - cta + 1, x.l, x.hk, x.base, x.row0, x.rows, 0, 0};
+                        }
+                        put(x);
+                        at += take;
+                        left -= take;
+                        in = 0;
+                    }
+                }
+            }
+        }
+        if (ok) put(Rec{});
+        if (lane == 0) {
+            if (!ok) join.parts = 0;
+            plan.join[cta] = join;
+        }
+    } else {
+        // ------------------------------------------------------------------------------- softmax, and what is written
+        const int wg = warp >> 2, quad = warp & 3, trow = quad * 32 + lane;      // lane of TMEM: row of this group's tile
+        const uint32_t tq = tmem + (uint32_t(quad * 32) << 16);
+        const float c2 = p.scale * 1.4426950408889634f;
+        uint32_t syncs = 0, cnt[2] = {0, 0};                 // items of each buffer in earlier segments
+        int16_t *par = reinterpret_cast<int16_t *>(smem + C::OffPar);
+        auto sync = [&]() -> bool {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(C::kSync));
+            return wait_fast(bar(C::kSync), syncs++ & 1, abort_flag);
+        };
+        for (uint32_t seg = 0; ok && record(seg, r); ++seg) {
+            const bool two = LANES == 2 && r.rows > 128;
+            const int tiles = r.t1 - r.t0;
+            const int n_buf[2] = {two ? tiles : (tiles + 1) / 2, two ? tiles : tiles / 2};
+            // everyone is through with the last segment: its queries, its parents, its sums
+            if (!(ok = sync())) break;
+            if (threadIdx.x == 0) topo_bad[(seg & 1) ^ 1] = 0;
+            {
+                const int chunks = r.rows * (D / 8);
+                for (int i = threadIdx.x; i < chunks; i += SOFT * 32) {
+                    const int row = i / (D / 8), c = i % (D / 8), at = r.row0 + row, node = at / group, g = at - node * group;
+                    const uint4 x = *reinterpret_cast<const uint4 *>(
+                        p.q + ((size_t(r.l) * p.T + r.base + node) * p.H + r.hk * group + g) * D + c * 8);
+                    const int tile = row >> 7, tr = row & 127;
+                    *reinterpret_cast<uint4 *>(smem + C::OffQ + tile * C::Q_BYTES + (c >> 3) * (128 * 128) + tr * 128 + (((c & 7) ^ (tr & 7)) << 4)) = x;
+                }
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(C::kQFull));
+            }
+            if (p.parent != nullptr && r.t1 > r.ct) {        // (a piece without draft keys is joined with one that looks)
+                int bad = 0;
+                for (int i = threadIdx.x; i < r.n; i += SOFT * 32) {
+                    const int up = p.parent[r.base + i];
+                    bad |= up < -1 || up >= i;
+                    par[i] = int16_t(up < -1 || up >= i ? -1 : up);
+                }
+                if (__any_sync(0xffffffffu, bad) && lane == 0) {
+                    topo_bad[seg & 1] = 1;
+                    atomicOr(p.status, SPECA_STATUS_BAD_PARENT);
+                }
+                if (!(ok = sync())) break;
+            }
+            const int row = (two ? wg * 128 : 0) + trow;     // row of the unit
+            const bool live = (two ? wg * 128 : 0) + quad * 32 < r.rows;     // the warp has rows
+            const int at = r.row0 + (row < r.rows ? row : 0), node = at / group, g = at - node * group;
+            float m = -INFINITY, l = 0.f;
+            const int items = LANES == 2 ? n_buf[wg] : tiles;
+#pragma unroll 1
+            for (int i = 0; i < items; ++i) {
+                // (one group has all items, alternately in the two buffers; two groups have a buffer each)
+                const int buf = LANES == 2 ? wg : i & 1;
+                const uint32_t k = LANES == 2 ? cnt[wg] + i : cnt[i & 1] + (i >> 1);         // items of that buffer so far
+                const int t = r.t0 + (LANES == 2 ? (two ? i : 2 * i + wg) : i);
+                if (!(ok = wait_fast(bar(C::kSFull + buf), k & 1, abort_flag))) break;
+                tc_fence_after();
+                if (live) {
+                    const uint32_t ta = tq + buf * N;
+                    float s[N];
+#pragma unroll
+                    for (int c = 0; c < N / 32; ++c) tmem_ld32(ta + 32 * c, s + 32 * c);
+                    tmem_ld_wait();
+                    const int valid = valid_of(r, t);
+                    if (t >= r.ct || valid < N) {
+                        uint32_t mask[N / 32];
+                        const int first = (t - r.ct) * N;    // first node of a draft tile
+                        if (t < r.ct || p.parent == nullptr) {
+                            const int upto = t < r.ct ? valid : node + 1 - first;
+#pragma unroll
+                            for (int w = 0; w < N / 32; ++w) {
+                                const int x = upto - 32 * w;
+                                mask[w] = x >= 32 ? 0xffffffffu : x <= 0 ? 0u : (1u << x) - 1u;
+                            }
+                        } else {
+#pragma unroll
+                            for (int w = 0; w < N / 32; ++w) mask[w] = 0u;
+                            for (int a = node; a >= first; a = par[a]) {
+                                const int x = a - first;
+#pragma unroll
+                                for (int w = 0; w < N / 32; ++w) mask[w] |= (x >> 5) == w ? 1u << (x & 31) : 0u;
+                            }
+                        }
+#pragma unroll
+                        for (int c = 0; c < N; ++c)
+                            if (!(mask[c >> 5] >> (c & 31) & 1u)) s[c] = -INFINITY;
+                    }
+                    float top4[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+                    for (int c = 4; c < N; ++c) top4[c & 3] = fmaxf(top4[c & 3], s[c]);
+                    const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
+                    if (i == 0) m = top;
+                    else if (__any_sync(0xffffffffu, (top - m) * c2 > kSlack || (m == -INFINITY && top > m))) {
+                        // the last item's product must have been added before O is scaled
+                        const int pb = LANES == 2 ? wg : (i - 1) & 1;
+                        const uint32_t pk = LANES == 2 ? k - 1 : cnt[pb] + ((i - 1) >> 1);
+                        if (!(ok = wait_fast(bar(C::kODone + pb), pk & 1, abort_flag))) break;
+                        tc_fence_after();
+                        const float now = fmaxf(m, top);
+                        // (before its first key a row's sums are zero, in whatever scale)
+                        const float f = m == now || m == -INFINITY ? 1.f : exp2_approx((m - now) * c2);
+                        m = now;
+                        l *= f;
+                        const uint32_t to = tq + kOCol + (LANES == 2 ? wg * D : 0);
+#pragma unroll 1
+                        for (int c = 0; c < D; c += 32) {
+                            float o[32];
+                            tmem_ld32(to + c, o);
+                            tmem_ld_wait();
+                            uint32_t x[16];
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) x[e] = __float_as_uint(o[16 * h + e] * f);
+                                tmem_st16(to + c + 16 * h, x);
+                            }
+                        }
+                        tmem_st_wait();
+                    }
+                    const float mc = m == -INFINITY ? 0.f : m * c2;
+                    float add[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int c = 0; c < N / 32; ++c) {
+                        uint32_t x[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const float a = exp2_approx(fmaf(s[32 * c + 2 * e], c2, -mc)), b = exp2_approx(fmaf(s[32 * c + 2 * e + 1], c2, -mc));
+                            add[(2 * e) & 3] += a;
+                            add[(2 * e + 1) & 3] += b;
+                            x[e] = pack_bf16(a, b);
+                        }
+                        tmem_st16(ta + 16 * c, x);
+                    }
+                    l += (add[0] + add[1]) + (add[2] + add[3]);
+                    tmem_st_wait();
+                    tc_fence_before();
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(C::kPReady + buf));
+            }
+            if (!ok) break;
+
+            // ---- end of the segment.  Sums of even and odd tiles: both groups read both, half of the columns each.
+            const bool merge = LANES == 2 && !two;
+            float f0 = 1.f, f1 = 0.f, mm = m, ll = l;
+            if (merge) {
+                float2 *ex = reinterpret_cast<float2 *>(smem + C::OffQ + C::Q_BYTES);        // (the second row tile's queries: there are none)
+                ex[wg * 128 + trow] = make_float2(m, l);
+                if (!(ok = sync())) break;
+                const float2 a = ex[trow], b = ex[128 + trow];
+                mm = fmaxf(a.x, b.x);
+                const float base = mm == -INFINITY ? 0.f : mm;
+                f0 = a.x == mm ? 1.f : exp2_approx((a.x - base) * c2);
+                f1 = b.x == mm ? 1.f : exp2_approx((b.x - base) * c2);
+                // (a maximum that is not a number belongs to sums that are not either)
+                ll = a.y * f0 + (n_buf[1] > 0 ? b.y * f1 : 0.f);
+            }
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const bool need = merge ? n_buf[b] > 0 : LANES == 2 ? b == wg : b == ((tiles - 1) & 1);
+                if (need && ok) ok = wait_fast(bar(C::kODone + b), (cnt[b] + n_buf[b] - 1) & 1, abort_flag);
+            }
+            if (!ok) break;
+            tc_fence_after();
+            const bool bad = topo_bad[seg & 1] != 0 && p.parent != nullptr && r.t1 > r.ct;
+            const bool skip = bad || page_bad[seg % kFlagRing] == int(seg) + 1;
+            const bool mend = value_bad[seg % kFlagRing] == int(seg) + 1;
+            if (live) {
+                const uint32_t o0 = tq + kOCol + (LANES == 2 && two ? wg * D : 0), o1 = tq + kOCol + D;
+                const bool both = merge && n_buf[1] > 0;
+                const int c_lo = merge ? wg * (D / 2) : 0, c_hi = merge ? c_lo + D / 2 : D;
+                const float inv = 1.f / ll;
+                float *sums = r.slot >= 0 ? slot_sums(plan, cta, r.slot) : nullptr;
+#pragma unroll 1
+                for (int c = c_lo; c < c_hi; c += 32) {
+                    float o[32];
+                    tmem_ld32(o0 + c, o);
+                    tmem_ld_wait();
+                    if (merge) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] *= f0;
+                        if (both) {
+                            float x[32];
+                            tmem_ld32(o1 + c, x);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) o[e] = fmaf(x[e], f1, o[e]);
+                        }
+                    }
+                    if (mend) {
+                        // draft values that are not finite, of the nodes that this row attends
+                        const int lo = r.t0 < r.ct ? 0 : (r.t0 - r.ct) * N, hi = (r.t1 - r.ct) * N;
+                        for (int a = node; a >= lo; a = p.parent != nullptr ? int(par[a]) : a - 1)
+                            if (a < hi) {
+                                const __nv_bfloat16 *v = p.v + ((size_t(r.l) * p.T + r.base + a) * p.HK + r.hk) * D + c;
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) {
+                                    const float x = __bfloat162float(v[e]);
+                                    if (!isfinite(x)) o[e] += x;
+                                }
+                            }
+                    }
+                    if (row < r.rows && !skip) {
+                        if (sums == nullptr) {
+                            uint4 *to = reinterpret_cast<uint4 *>(p.o + ((size_t(r.l) * p.T + r.base + node) * p.H + r.hk * group + g) * D + c);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                to[e] = make_uint4(pack_bf16(o[8 * e] * inv, o[8 * e + 1] * inv), pack_bf16(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
+                                                   pack_bf16(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_bf16(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
+                        } else {
+                            float4 *to = reinterpret_cast<float4 *>(sums + size_t(row) * D + c);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) to[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                        }
+                    }
+                }
+                if (sums != nullptr) {
+                    float *tail = sums + size_t(plan.rows_cap) * D;
+                    if (row < r.rows && c_lo == 0) reinterpret_cast<float2 *>(tail)[row] = make_float2(mm, ll);
+                    if (row == 0 && c_lo == 0) reinterpret_cast<int *>(tail + 2 * plan.rows_cap)[0] = skip;
+                }
+            }
+            tc_fence_before();
+            cnt[0] += n_buf[0];
+            cnt[1] += n_buf[1];
+        }
     }
-    for (int a = t - base; a >= 0; a = p.parent != nullptr ? p.parent[base + a] : a - 1) {
-        const size_t at = (size_t(l) * p.T + base + a) * p.HK + hk;
-        take(p.k + at * D, p.v + at * D);
+
+    if (warp == SOFT + 1) {
+        // everything this warp issued must have completed before TMEM is released
+        mma_commit(bar(C::kDrain), lead);
+        mbar_wait(bar(C::kDrain), 0, abort_flag);
     }
-    for (int i = 0; i < E; ++i) p.o[row * D + lane + 32 * i] = __float2bfloat16_rn(o[i] / sum);
+    if (warp == SOFT && *abort_flag) {
+        // let copies still in flight land before the CTA's shared memory goes away
+        const uint64_t t0 = global_timer_ns();
+        while (global_timer_ns() - t0 < 200000ull) __nanosleep(1000);
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (threadIdx.x == 0 && *abort_flag) {
+        atomicOr(p.status, SPECA_STATUS_TIMEOUT);
+        plan.join[cta].parts = 0;
+    }
+    if (warp == SOFT + 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, kTmemCols);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// Units that several CTAs have a piece of: a warp a row, pieces in order, so that the result does not depend on which CTA
+// was ready first.
+// ---------------------------------------------------------------------------------------------------------------
+constexpr int kJoinWarps = 8;
+
+template <int D>
+__global__ void __launch_bounds__(kJoinWarps * 32)
+join_kernel(AttnParams p, Plan plan, int32_t blocks)
+{
+    after_previous_kernel();
+    const int cta = blockIdx.x / blocks, lane = threadIdx.x & 31;
+    const Join j = plan.join[cta];
+    const int row = (blockIdx.x % blocks) * kJoinWarps + (threadIdx.x >> 5);
+    if (j.parts <= 1 || row >= j.rows) return;
+    const float c2 = p.scale * 1.4426950408889634f;
+    auto tail = [&](int i) { return slot_sums(plan, cta + i, i == 0 ? 1 : 0) + size_t(plan.rows_cap) * D; };
+    float m = -INFINITY;
+    int skip = 0;
+    for (int i = lane; i < j.parts; i += 32) {
+        m = fmaxf(m, reinterpret_cast<const float2 *>(tail(i))[row].x);
+        skip |= reinterpret_cast<const int *>(tail(i) + 2 * plan.rows_cap)[0];
+    }
+#pragma unroll
+    for (int w = 16; w > 0; w /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
+    if (__any_sync(0xffffffffu, skip)) return;
+    constexpr int E = D / 32;
+    float o[E], l = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = 0.f;
+#pragma unroll 2
+    for (int i = 0; i < j.parts; ++i) {
+        const float2 ml = reinterpret_cast<const float2 *>(tail(i))[row];
+        const float f = ml.x == m ? 1.f : exp2_approx((ml.x - m) * c2);
+        const float *x = slot_sums(plan, cta + i, i == 0 ? 1 : 0) + size_t(row) * D + lane * E;
+        l = fmaf(ml.y, f, l);
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = fmaf(x[e], f, o[e]);
+    }
+    const int group = p.H / p.HK, at = j.row0 + row, node = at / group, g = at % group;
+    __nv_bfloat16 *to = p.o + ((size_t(j.l) * p.T + j.base + node) * p.H + j.hk * group + g) * D + lane * E;
+    const float inv = 1.f / l;
+#pragma unroll
+    for (int e = 0; e < E; e += 2) *reinterpret_cast<uint32_t *>(to + e) = pack_bf16(o[e] * inv, o[e + 1] * inv);
+}
+
+std::atomic<bool> g_opted_in[64];                            // per device: shared memory of every instantiation
+
+template <int D> int launch_width(const AttnParams &p, cudaStream_t st)
+{
+    using C = Cfg<D>;
+    EncodeTiledFn encode = encode_tiled_fn();
+    if (encode == nullptr) return int(cudaErrorNotSupported);
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return int(cudaErrorInvalidDevice);
+    const int sms = sm_count_of_current_device();
+    if (sms <= 0) return int(cudaErrorInvalidDevice);
+    if (!g_opted_in[dev].load(std::memory_order_acquire)) {
+        cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void *>(attend_kernel<64>), cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<64>::Bytes);
+        if (e == cudaSuccess)
+            e = cudaFuncSetAttribute(reinterpret_cast<const void *>(attend_kernel<128>), cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<128>::Bytes);
+        if (e == cudaSuccess)
+            e = cudaFuncSetAttribute(reinterpret_cast<const void *>(attend_kernel<256>), cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<256>::Bytes);
+        if (e != cudaSuccess) return int(e);
+        g_opted_in[dev].store(true, std::memory_order_release);
+    }
+    const int page = 1 << p.page_shift, box_rows = page < C::N ? page : C::N;
+    CUtensorMap maps[4];
+    const cuuint32_t es[3] = {1, 1, 1};
+    for (int i = 0; i < 4; ++i) {
+        const bool cache = i < 2;
+        const void *base = i == 0 ? p.k_cache : i == 1 ? p.v_cache : i == 2 ? p.k : p.v;
+        const cuuint64_t dim[3] = {cuuint64_t(D), cuuint64_t(cache ? page : p.HK),
+                                   cache ? cuuint64_t(p.L) * p.n_pages * p.HK : cuuint64_t(p.L) * p.T};
+        const cuuint64_t stride[2] = {cuuint64_t(D) * 2, dim[1] * D * 2};
+        const cuuint32_t box[3] = {64, cuuint32_t(cache ? box_rows : 1), cuuint32_t(cache ? 1 : 16)};
+        if (encode(&maps[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dim, stride, box, es,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return int(cudaErrorInvalidValue);
+    }
+    Plan plan;
+    plan.rows_cap = slot_rows(p.max_nodes, p.H / p.HK, C::MT);
+    plan.slot_bytes = slot_bytes(plan.rows_cap, D);
+    plan.join = static_cast<Join *>(p.workspace);
+    plan.slots = static_cast<char *>(p.workspace) + align256(sizeof(Join) * kMaxCtas);
+    const int grid = sms < kMaxCtas ? sms : kMaxCtas;
+    launch(attend_kernel<D>, grid, C::THREADS, C::Bytes, st, maps[0], maps[1], maps[2], maps[3], p, plan, int32_t(box_rows));
+    const int e = int(cudaGetLastError());
+    if (e != 0) return e;
+    const int blocks = (plan.rows_cap + kJoinWarps - 1) / kJoinWarps;
+    launch(join_kernel<D>, unsigned(grid * blocks), kJoinWarps * 32, 0, st, p, plan, int32_t(blocks));
+    return int(cudaGetLastError());
 }
 
 }  // namespace
 
 size_t attend_workspace_bytes(const speca_attn_dims *d)
 {
-    (void)d;
-    return 16;
+    const int mt = d->d_head == 256 ? Cfg<256>::MT : Cfg<128>::MT;
+    return align256(sizeof(Join) * kMaxCtas) + 2 * kMaxCtas * slot_bytes(slot_rows(d->max_nodes, d->heads / d->kv_heads, mt), d->d_head);
 }
 
 int launch_attend(const AttnParams &p, int d_head, cudaStream_t st)
 {
-    const long blocks = (long(p.L) * p.T * p.H + kWarps - 1) / kWarps;
-    if (blocks > 0x7fffffffL) return int(cudaErrorInvalidConfiguration);
-    if (d_head == 64) launch(attend_kernel<64>, unsigned(blocks), kWarps * 32, 0, st, p);
-    else if (d_head == 128) launch(attend_kernel<128>, unsigned(blocks), kWarps * 32, 0, st, p);
-    else launch(attend_kernel<256>, unsigned(blocks), kWarps * 32, 0, st, p);
-    return int(cudaGetLastError());
+    if (d_head == 64) return launch_width<64>(p, st);
+    if (d_head == 128) return launch_width<128>(p, st);
+    return launch_width<256>(p, st);
 }
 
 }  // namespace speca
