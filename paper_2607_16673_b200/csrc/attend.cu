@@ -142,6 +142,12 @@ __device__ __forceinline__ float exp2_approx(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
+// 16 bytes from global to shared memory, none of a thread's copies waits for another
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy16_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 __device__ __forceinline__ bool not_finite(uint32_t pair)
 {
     return (pair & 0x7f80u) == 0x7f80u || (pair & 0x7f800000u) == 0x7f800000u;
@@ -516,11 +522,11 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
                 const int chunks = r.rows * (D / 8);
                 for (int i = threadIdx.x; i < chunks; i += SOFT * 32) {
                     const int row = i / (D / 8), c = i % (D / 8), at = r.row0 + row, node = at / group, g = at - node * group;
-                    const uint4 x = *reinterpret_cast<const uint4 *>(
-                        p.q + ((size_t(r.l) * p.T + r.base + node) * p.H + r.hk * group + g) * D + c * 8);
                     const int tile = row >> 7, tr = row & 127;
-                    *reinterpret_cast<uint4 *>(smem + C::OffQ + tile * C::Q_BYTES + (c >> 3) * (128 * 128) + tr * 128 + (((c & 7) ^ (tr & 7)) << 4)) = x;
+                    copy16(sbase + C::OffQ + tile * C::Q_BYTES + (c >> 3) * (128 * 128) + tr * 128 + (((c & 7) ^ (tr & 7)) << 4),
+                           p.q + ((size_t(r.l) * p.T + r.base + node) * p.H + r.hk * group + g) * D + c * 8);
                 }
+                copy16_wait();
                 fence_proxy_async();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(C::kQFull));

@@ -6,29 +6,18 @@ namespace speca {
 namespace {
 
 // ---------------------------------------------------------------------------------------------------------------
-// Norm and rotation.  A warp takes a share of one token's head rows over all layers: a lane has 8 consecutive elements (16
-// bytes) of a row, D / 8 lanes a row, so its angles are the same for every row of the token and are formed once.
+// Norm and rotation.  A warp takes a share of one token's head rows over all layers.  D / 8 lanes have a row, and a lane has both
+// elements of four pairs (lanes beyond the rotated part: eight plain elements), so no element travels between lanes but for
+// the sum of squares, and its four angles are the same for every row of the token: they are formed once.  Weights, cosines and
+// sines of a layer's queries (or keys) are multiplied out beforehand, which leaves eight products, eight fused multiply-adds
+// and the scale by the norm a row.  The rows of the next step are asked for before this one's are worked on.
 // ---------------------------------------------------------------------------------------------------------------
-constexpr int kNormWarps = 8;
+constexpr int kNormWarps = 4, kNormRows = 4;                // rows a lane has in flight
 
-__device__ __forceinline__ void unpack8(const uint4 &x, float (&f)[8])
+__device__ __forceinline__ uint32_t pack2(float lo, float hi)
 {
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        f[2 * i] = __uint_as_float(w[i] << 16);
-        f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-}
-__device__ __forceinline__ uint4 pack8(const float (&f)[8])
-{
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-        w[i] = *reinterpret_cast<const uint32_t *>(&h);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
 }
 
 // Sequence of packed node t, whole warp: the number of sequences that end at or before it (B if there is none).
@@ -39,24 +28,51 @@ __device__ __forceinline__ int sequence_of(const int32_t *node_offsets, int B, i
     return __reduce_add_sync(0xffffffffu, before);
 }
 
-template <int D>
+template <int D, bool INTER>
 __global__ void __launch_bounds__(kNormWarps * 32)
 norm_rope_kernel(AttnParams p, NormParams np, int32_t parts)
 {
     after_previous_kernel();
-    constexpr int LPH = D / 8, HPW = 32 / LPH;             // lanes of a row, rows a warp has at a time
-    const int lane = threadIdx.x & 31;
+    constexpr int LPH = D / 8, HPW = 32 / LPH, U = kNormRows;      // lanes of a row, rows a warp has side by side
+    const int lane = threadIdx.x & 31, sub = lane / LPH, in = lane % LPH;
     const long task = long(blockIdx.x) * kNormWarps + (threadIdx.x >> 5);
     const int t = int(task / parts), part = int(task % parts);
     if (t >= p.T) return;
-    const int b = sequence_of(p.node_offsets, p.B, t, lane);
+    // this lane's elements of a row: ea .. ea + 3 and eb .. eb + 3
+    const int half = np.rot / 2;
+    const bool turned = 8 * in < np.rot;
+    const int ea = !INTER && turned ? 4 * in : 8 * in, eb = !INTER && turned ? half + 4 * in : 8 * in + 4;
+
+    const int steps_q = (p.H + HPW - 1) / HPW, steps = steps_q + (p.HK + HPW - 1) / HPW;
+    const long total = long(p.L) * steps, per = (total + parts - 1) / parts;
+    long it = part * per;
+    const long end = min(total, it + per);
+    int l = int(it / steps), s = int(it % steps);
+    // up to U steps from (l, s) on, of the queries or of the keys of one layer
+    auto width = [&](long it, int s) { return int(min(long(min(U, (s < steps_q ? steps_q : steps) - s)), end - it)); };
+    auto ask = [&](int l, int s, int m, uint2 (&a)[U], uint2 (&b)[U]) {
+        const bool is_q = s < steps_q;
+        const __nv_bfloat16 *row = is_q ? p.q + l * np.q_layer + t * np.q_token : p.k + l * np.k_layer + t * np.k_token;
+        const int h0 = (is_q ? s : s - steps_q) * HPW + sub, heads = is_q ? p.H : p.HK;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (u < m && h0 + u * HPW < heads) {
+                a[u] = *reinterpret_cast<const uint2 *>(row + (h0 + u * HPW) * D + ea);
+                b[u] = *reinterpret_cast<const uint2 *>(row + (h0 + u * HPW) * D + eb);
+            } else a[u] = b[u] = make_uint2(0u, 0u);
+    };
+    uint2 a[U], b[U];
+    int m = width(it, s);
+    if (it < end) ask(l, s, m, a, b);
+
+    const int seq = sequence_of(p.node_offsets, p.B, t, lane);
     int base, n, fault = 0;
-    if (b >= p.B) fault = SPECA_STATUS_BAD_OFFSETS;        // behind the last sequence
-    else fault = sequence_nodes(p, b, base, n);
+    if (seq >= p.B) fault = SPECA_STATUS_BAD_OFFSETS;      // behind the last sequence
+    else fault = sequence_nodes(p, seq, base, n);
     if (!fault && t < base) fault = SPECA_STATUS_BAD_OFFSETS;
     int depth = 0, len = 0;
     if (!fault) {
-        len = p.kv_len[b];
+        len = p.kv_len[seq];
         if (len < 0) fault = SPECA_STATUS_BAD_PAGE;
         if (p.parent == nullptr) depth = t - base + 1;
         else {
@@ -67,81 +83,90 @@ norm_rope_kernel(AttnParams p, NormParams np, int32_t parts)
             }
             if (__any_sync(0xffffffffu, bad)) fault |= SPECA_STATUS_BAD_PARENT;
             else
-                for (int a = t - base; a >= 0; a = p.parent[base + a]) ++depth;
+                for (int x = t - base; x >= 0; x = p.parent[base + x]) ++depth;
         }
     }
     if (fault) {
         if (lane == 0 && part == 0) atomicOr(p.status, fault);
         return;
     }
-
-    // this lane's 8 elements of a row, and for each the element it is rotated with
-    const int e0 = (lane % LPH) * 8, half = np.rot / 2;
-    const bool turned = e0 < np.rot;
-    int mate = lane;                                        // lane that has the other elements of the pairs (itself: interleaved)
-    if (turned && !np.interleaved) mate = e0 < half ? lane + half / 8 : lane - half / 8;
-    float c[8], s[8];                                       // element <- element * c + partner * s
+    float cs[4], sn[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { c[i] = 1.f; s[i] = 0.f; }
+    for (int i = 0; i < 4; ++i) { cs[i] = 1.f; sn[i] = 0.f; }
     if (turned) {
         const double pos = double(len) + double(depth - 1);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int e = e0 + i;
-            const int j = np.interleaved ? e / 2 : (e < half ? e : e - half);
-            const bool first = np.interleaved ? (e & 1) == 0 : e < half;
+        for (int i = 0; i < 4; ++i) {
             // the angle in turns, whole ones taken off in 64 bits: far positions leave fp32 no digits behind the point
-            const double turns = pos * double(np.inv_freq[j]) * 0.15915494309189533577;
-            float sn, cs;
-            sincospif(2.f * float(turns - rint(turns)), &sn, &cs);
-            c[i] = cs * np.rope_scale;
-            s[i] = (first ? -sn : sn) * np.rope_scale;
+            const double turns = pos * double(np.inv_freq[4 * in + i]) * 0.15915494309189533577;
+            sincospif(2.f * float(turns - rint(turns)), &sn[i], &cs[i]);
+            cs[i] *= np.rope_scale;
+            sn[i] *= np.rope_scale;
         }
     }
 
-    const int rows = p.H + p.HK, steps = (rows + HPW - 1) / HPW;
-    const long total = long(p.L) * steps, per = (total + parts - 1) / parts;
-    const long end = min(total, (part + 1) * per);
-    for (long it = part * per; it < end; ++it) {
-        const int l = int(it / steps), r = int(it % steps) * HPW + lane / LPH;
-        const bool on = r < rows, is_q = r < p.H;
-        const int h = is_q ? r : r - p.H;
-        uint4 raw = make_uint4(0u, 0u, 0u, 0u);
-        if (on) {
-            const __nv_bfloat16 *row = is_q ? p.q + l * np.q_layer + t * np.q_token : p.k + l * np.k_layer + t * np.k_token;
-            raw = *reinterpret_cast<const uint4 *>(row + h * D + e0);
-        }
-        float x[8], y[8];
-        unpack8(raw, x);
+    // first <- first * k0 - second * k1, second <- first * k2 + second * k3 of pair i, before the norm's scale
+    float k0[4], k1[4], k2[4], k3[4];
+    int made = -1;                                          // 2 * layer + (keys) that they are for
+    while (it < end) {
+        const bool is_q = s < steps_q;
+        // what comes after this step
+        const long it2 = it + m;
+        const int s2 = s + m == steps ? 0 : s + m, l2 = s + m == steps ? l + 1 : l, m2 = it2 < end ? width(it2, s2) : 0;
+        uint2 a2[U], b2[U];
+        if (m2 > 0) ask(l2, s2, m2, a2, b2);
         const float *w = is_q ? np.q_weight : np.k_weight;
-        float rs = 1.f;
-        if (np.q_weight != nullptr || np.k_weight != nullptr) {
-            float sum = 0.f;
+        if (made != 2 * l + !is_q) {
+            made = 2 * l + !is_q;
+            float4 wa = make_float4(1.f, 1.f, 1.f, 1.f), wb = wa;
+            if (w != nullptr) {
+                wa = *reinterpret_cast<const float4 *>(w + size_t(l) * D + ea);
+                wb = *reinterpret_cast<const float4 *>(w + size_t(l) * D + eb);
+            }
+            const float x[8] = {wa.x, wa.y, wa.z, wa.w, wb.x, wb.y, wb.z, wb.w};
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], sum);
-#pragma unroll
-            for (int m = LPH / 2; m > 0; m /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, m);
-            if (w != nullptr) rs = rsqrtf(sum * (1.f / D) + np.eps);
+            for (int i = 0; i < 4; ++i) {
+                const float f = INTER ? x[2 * i] : x[i], g = INTER ? x[2 * i + 1] : x[4 + i];
+                k0[i] = f * cs[i]; k1[i] = g * sn[i]; k2[i] = f * sn[i]; k3[i] = g * cs[i];
+            }
         }
-        if (w != nullptr && on) {
-            const float4 *w4 = reinterpret_cast<const float4 *>(w + size_t(l) * D + e0);
-            const float4 a = w4[0], d = w4[1];
-            const float ww[8] = {a.x, a.y, a.z, a.w, d.x, d.y, d.z, d.w};
+        const int h0 = (is_q ? s : s - steps_q) * HPW + sub, heads = is_q ? p.H : p.HK;
+        __nv_bfloat16 *out = (is_q ? np.q_out : np.k_out) + (size_t(l) * p.T + t) * heads * D;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = x[i] * rs * ww[i];
-        }
+        for (int u = 0; u < U; ++u)
+            if (u < m) {
+                const uint32_t raw[4] = {a[u].x, a[u].y, b[u].x, b[u].y};
+                float x[8], y[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float other = __shfl_sync(0xffffffffu, x[i], mate);
-            y[i] = np.interleaved ? x[i ^ 1] : other;
-        }
-        if (turned)
+                for (int i = 0; i < 4; ++i) {
+                    x[2 * i] = __uint_as_float(raw[i] << 16);
+                    x[2 * i + 1] = __uint_as_float(raw[i] & 0xffff0000u);
+                }
+                float rs = 1.f;
+                if (w != nullptr) {
+                    float sum = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = x[i] * c[i] + y[i] * s[i];
-        if (on) {
-            __nv_bfloat16 *out = is_q ? np.q_out + (size_t(l) * p.T + t) * p.H * D : np.k_out + (size_t(l) * p.T + t) * p.HK * D;
-            *reinterpret_cast<uint4 *>(out + size_t(h) * D + e0) = pack8(x);
-        }
+                    for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], sum);
+#pragma unroll
+                    for (int j = LPH / 2; j > 0; j /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, j);
+                    rs = rsqrtf(sum * (1.f / D) + np.eps);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int e = INTER ? 2 * i : i, f = INTER ? 2 * i + 1 : 4 + i;
+                    // (a plain element takes nothing from its neighbour, not even what is not finite)
+                    y[e] = turned ? fmaf(x[e], k0[i], -(x[f] * k1[i])) * rs : x[e] * k0[i] * rs;
+                    y[f] = turned ? fmaf(x[e], k2[i], x[f] * k3[i]) * rs : x[f] * k3[i] * rs;
+                }
+                if (h0 + u * HPW < heads) {
+                    __nv_bfloat16 *to = out + size_t(h0 + u * HPW) * D;
+                    *reinterpret_cast<uint2 *>(to + ea) = make_uint2(pack2(y[0], y[1]), pack2(y[2], y[3]));
+                    *reinterpret_cast<uint2 *>(to + eb) = make_uint2(pack2(y[4], y[5]), pack2(y[6], y[7]));
+                }
+            }
+        it = it2; s = s2; l = l2; m = m2;
+#pragma unroll
+        for (int u = 0; u < U; ++u) { a[u] = a2[u]; b[u] = b2[u]; }
     }
 }
 
@@ -287,15 +312,19 @@ int launch_norm_rope(const AttnParams &p, const NormParams &n, int d_head, cudaS
 {
     const long sms = sm_count_of_current_device();
     if (sms <= 0) return int(cudaErrorInvalidDevice);
-    const long steps = long(p.L) * ((p.H + p.HK) * (d_head / 8) + 31) / 32, most = sms * 64;
-    long parts = p.T >= most ? 1 : most / p.T;
+    const int hpw = 256 / d_head;
+    const long steps = long(p.L) * ((p.H + hpw - 1) / hpw + (p.HK + hpw - 1) / hpw);
+    // A token's rows stay with one warp, which then forms its angles once, as long as that makes enough warps to fill the
+    // machine; a few tokens are spread over as many warps as they have steps.
+    const long most = sms * 64;
+    long parts = p.T >= most ? 1 : (most + p.T - 1) / p.T;
     if (parts > steps) parts = steps;
     unsigned grid;
     const int rc = grid_of((p.T * parts + kNormWarps - 1) / kNormWarps, grid);
     if (rc != 0) return rc;
-    if (d_head == 64) launch(norm_rope_kernel<64>, grid, kNormWarps * 32, 0, st, p, n, int(parts));
-    else if (d_head == 128) launch(norm_rope_kernel<128>, grid, kNormWarps * 32, 0, st, p, n, int(parts));
-    else launch(norm_rope_kernel<256>, grid, kNormWarps * 32, 0, st, p, n, int(parts));
+    auto go = [&](auto kernel) { launch(kernel, grid, kNormWarps * 32, 0, st, p, n, int(parts)); };
+    if (n.interleaved) go(d_head == 64 ? norm_rope_kernel<64, true> : d_head == 128 ? norm_rope_kernel<128, true> : norm_rope_kernel<256, true>);
+    else go(d_head == 64 ? norm_rope_kernel<64, false> : d_head == 128 ? norm_rope_kernel<128, false> : norm_rope_kernel<256, false>);
     return int(cudaGetLastError());
 }
 
