@@ -24,25 +24,28 @@ constexpr int kRecords = 4;              // ring of segment records
 constexpr float kSlack = 8.f;            // binary digits a maximum may grow by before O is scaled
 constexpr int kFlagRing = 8;
 
-// D <= 128: two softmax groups of 128 rows, each with an O of its own.  A unit of at most 128 rows has its even key tiles in
-// one and the odd ones in the other, joined at the end; a larger one has a row tile in each, over the same keys.  D = 256: O
-// alone takes half of TMEM; one group, and S of the next tile is formed while it works on this one.
+// D <= 128: two softmax groups of 128 rows, each with an O and a buffer for S of its own.  A unit of at most 128 rows has its
+// even key tiles in one and the odd ones in the other, joined at the end; a larger one has a row tile in each, over the same
+// keys.  D = 256: O alone takes half of TMEM, and there is one group, over tiles of half as many keys in three buffers.
+// P takes the first half of the columns of its S.  One warp asks for scores, another for the products with V, so that neither's waits
+// hold the other up (a loop over one item takes 1200 cycles beside its 12 products where one warp does both).
 template <int D> struct Cfg {
     static constexpr int N = D == 256 ? 64 : 128;
     static constexpr int LANES = D == 256 ? 1 : 2;
+    static constexpr int BUFS = LANES == 2 ? 2 : 3;
     static constexpr int MT = 128 * LANES;
-    static constexpr int SOFT = 4 * LANES;                   // softmax warps; then TMA, MMA, mending of V, schedule
-    static constexpr int THREADS = (SOFT + 4) * 32;
+    static constexpr int SOFT = 4 * LANES;                   // softmax warps; then TMA, scores, products with V, mending of V, schedule
+    static constexpr int THREADS = (SOFT + 5) * 32;
     static constexpr int Q_BYTES = 128 * D * 2;
     static constexpr int TILE = N * D * 2;                   // keys or values of a tile
-    static constexpr int SLOTS = D == 64 ? 10 : 5;
+    static constexpr int KS = D == 64 ? 5 : 2, VS = D == 64 ? 5 : 3;       // tiles of keys and of values in flight or in use
     static constexpr int OffQ = 0;
     static constexpr int OffRing = LANES * Q_BYTES;
-    static constexpr int OffPar = OffRing + SLOTS * TILE;    // int16 parent[kAttnMaxTree]; scratch of the scan before that
+    static constexpr int OffPar = OffRing + (KS + VS) * TILE;    // int16 parent[kAttnMaxTree]; scratch of the scan before that
     static constexpr int OffRec = OffPar + 2 * kAttnMaxTree;
     static constexpr int OffBars = OffRec + 64 * kRecords;
-    static constexpr int kFull = 0, kEmpty = SLOTS, kRaw = 2 * SLOTS, kSFull = 3 * SLOTS, kPReady = kSFull + 2, kODone = kPReady + 2,
-                         kQFull = kODone + 2, kSync = kQFull + 1, kRecFull = kSync + 1, kRecEmpty = kRecFull + kRecords,
+    static constexpr int kKFull = 0, kKEmpty = KS, kVFull = 2 * KS, kVEmpty = kVFull + VS, kVRaw = kVEmpty + VS, kSFull = kVRaw + VS, kPReady = kSFull + BUFS, kODone = kPReady + BUFS,
+                         kQFull = kODone + BUFS, kSync = kQFull + 1, kRecFull = kSync + 1, kRecEmpty = kRecFull + kRecords,
                          kDrain = kRecEmpty + kRecords, kBars = kDrain + 1;
     static constexpr int OffMisc = OffBars + 8 * kBars;      // abort, TMEM base, bad topology [2], start of the piece [4]
     static constexpr int OffFlags = OffMisc + 64;            // segment numbers: bad page [8], values that are not finite [8]
@@ -50,7 +53,7 @@ template <int D> struct Cfg {
 };
 static_assert(Cfg<128>::Bytes <= 232448 && Cfg<256>::Bytes <= 232448 && Cfg<64>::Bytes <= 232448, "shared memory of a CTA");
 
-constexpr int kTmemCols = 512, kOCol = 256;                  // S (P) buffers at 0 and N, O from column 256
+constexpr int kTmemCols = 512, kOCol = 256;                  // S (P) buffers from 0, N columns each, O from column 256
 
 // A piece of one unit: key tiles t0 .. t1-1, of which the first `ct` of the unit are the cache's.
 struct Rec {
@@ -97,6 +100,18 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float *r)
 #pragma unroll
     for (int i = 0; i < 32; ++i) r[i] = __uint_as_float(x[i]);
 }
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float *r)
+{
+    uint32_t x[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7]), "=r"(x[8]), "=r"(x[9]),
+          "=r"(x[10]), "=r"(x[11]), "=r"(x[12]), "=r"(x[13]), "=r"(x[14]), "=r"(x[15])
+        : "r"(taddr)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r[i] = __uint_as_float(x[i]);
+}
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&x)[16])
 {
     asm volatile(
@@ -104,6 +119,14 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&x)[16
         ::"r"(taddr), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]), "r"(x[8]),
           "r"(x[9]), "r"(x[10]), "r"(x[11]), "r"(x[12]), "r"(x[13]), "r"(x[14]), "r"(x[15])
         : "memory");
+}
+__device__ __forceinline__ void tmem_st2(uint32_t taddr, float x, float y)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1, %2};" ::"r"(taddr), "f"(x), "f"(y) : "memory");
+}
+__device__ __forceinline__ void tmem_ld2(uint32_t taddr, float2 &x)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x2.b32 {%0, %1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // kind::f16 (bf16) with the A operand in TMEM: a 32-bit column holds two consecutive K elements, the even one low
@@ -118,17 +141,42 @@ __device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, ui
         ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(lead)
         : "memory");
 }
-// MN-major operand (rows are K, 128 bytes of MN a row), 128-byte swizzle: `block` bytes from one 64-wide block of MN to the
-// next, 1024 from one group of eight rows to the next
-__device__ __forceinline__ uint64_t make_desc_mn(uint32_t smem_addr, uint32_t block)
+// A tile of keys or values in shared memory: groups of eight rows, in a group one 64-wide block of columns behind the other,
+// in a block eight rows of 128 bytes with the 128-byte swizzle.  So one copy brings a page whatever its width (with the blocks
+// outermost it takes one a block, and 32 copies a tile of 16-row pages and 128 columns took longer than the tile's bytes).
+template <int D> __device__ __forceinline__ uint32_t tile_offset(int row, int chunk)       // of 16 bytes
 {
-    uint64_t d = 0;
-    d |= uint64_t((smem_addr >> 4) & 0x3fffu);
-    d |= uint64_t((block >> 4) & 0x3fffu) << 16;
-    d |= uint64_t(1024 >> 4) << 32;
-    d |= uint64_t(1) << 46;
-    d |= uint64_t(2) << 61;
-    return d;
+    return uint32_t((row >> 3) * (D / 64) + (chunk >> 3)) * 1024u + (row & 7) * 128 + (((chunk & 7) ^ (row & 7)) << 4);
+}
+// operand whose rows are M or N (keys of S = Q K^T), `group` bytes between groups of eight rows
+__device__ __forceinline__ uint64_t make_desc_k(uint32_t smem_addr, uint32_t group)
+{
+    return (make_desc(smem_addr) & ~(uint64_t(0x3fff) << 32)) | uint64_t((group >> 4) & 0x3fffu) << 32;
+}
+// operand whose rows are K (values of O = P V): 1024 bytes from one 64-wide block of columns to the next, `group` between
+// groups of eight rows
+__device__ __forceinline__ uint64_t make_desc_mn(uint32_t smem_addr, uint32_t group)
+{
+    return (make_desc_k(smem_addr, group) & ~(uint64_t(0x3fff) << 16)) | uint64_t(1024 >> 4) << 16;
+}
+// as tma_load_3d, by the lane that has `lead` set
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int w, uint32_t bar, uint32_t lead)
+{
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "setp.ne.b32 q, %7, 0;\n\t"
+        "@q cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}"
+        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar), "r"(lead)
+        : "memory");
+}
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int w, int v, uint32_t bar, uint32_t lead)
+{
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "setp.ne.b32 q, %8, 0;\n\t"
+        "@q cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];\n\t}"
+        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(v), "r"(bar), "r"(lead)
+        : "memory");
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 {
@@ -140,6 +188,32 @@ __device__ __forceinline__ float exp2_approx(float x)
 {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// two fp32 values in a pair of registers, one instruction for both
+__device__ __forceinline__ uint64_t pair2(float lo, float hi)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpair2(uint64_t x, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
 // 16 bytes from global to shared memory, none of a thread's copies waits for another
@@ -199,7 +273,7 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
 {
     after_previous_kernel();
     using C = Cfg<D>;
-    constexpr int N = C::N, LANES = C::LANES, SOFT = C::SOFT, SLOTS = C::SLOTS;
+    constexpr int N = C::N, LANES = C::LANES, BUFS = C::BUFS, SOFT = C::SOFT, KS = C::KS, VS = C::VS;
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t sbase = smem_u32(smem);
     if (sbase & 1023u) {                                     // never expected; refuse to run rather than corrupt
@@ -221,12 +295,13 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
         *abort_flag = 0;
         topo_bad[0] = topo_bad[1] = 0;
         for (int i = 0; i < 2 * kFlagRing; ++i) page_bad[i] = 0;
-        for (int i = 0; i < SLOTS; ++i) { mbar_init(bar(C::kFull + i), 1); mbar_init(bar(C::kEmpty + i), 1); mbar_init(bar(C::kRaw + i), 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(bar(C::kSFull + i), 1); mbar_init(bar(C::kPReady + i), 4); mbar_init(bar(C::kODone + i), 1); }
+        for (int i = 0; i < KS; ++i) { mbar_init(bar(C::kKFull + i), 1); mbar_init(bar(C::kKEmpty + i), 1); }
+        for (int i = 0; i < VS; ++i) { mbar_init(bar(C::kVFull + i), 1); mbar_init(bar(C::kVEmpty + i), 1); mbar_init(bar(C::kVRaw + i), 1); }
+        for (int i = 0; i < BUFS; ++i) { mbar_init(bar(C::kSFull + i), 1); mbar_init(bar(C::kPReady + i), 4); mbar_init(bar(C::kODone + i), 1); }
         mbar_init(bar(C::kQFull), SOFT);
         mbar_init(bar(C::kSync), SOFT);
-        for (int i = 0; i < kRecords; ++i) { mbar_init(bar(C::kRecFull + i), 1); mbar_init(bar(C::kRecEmpty + i), SOFT + 3); }
-        mbar_init(bar(C::kDrain), 1);
+        for (int i = 0; i < kRecords; ++i) { mbar_init(bar(C::kRecFull + i), 1); mbar_init(bar(C::kRecEmpty + i), SOFT + 4); }
+        mbar_init(bar(C::kDrain), 2);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == SOFT + 1) tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_slot)), kTmemCols);
@@ -291,139 +366,155 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
         const int left = t < r.ct ? r.len - t * N : r.nodes - (t - r.ct) * N;
         return left < N ? left : N;
     };
-    // whose values are looked over before they are used: they land on a barrier of their own (the warp that does it skips the
-    // other tiles, so it could not tell two phases of the common barrier apart)
+    // (A barrier has two parities: whoever waits on one waits for all its phases in turn.  So keys and values have rings of
+    // their own, and values that are looked over before they are used land on a barrier of their own.)
     auto to_mend = [&](const Rec &r, int t) { return t >= r.ct || (valid_of(r, t) & 15) != 0; };
+    // Buffer of item i of a segment.  Every use of a buffer is one phase of its three barriers (scores there, weights there,
+    // weights used); a role keeps the parity of the next one, a bit a buffer.
+    auto buffer = [](int i) { return LANES == 2 ? i & 1 : i % 3; };
     Rec r;
 
     if (warp == SOFT) {
         // ------------------------------------------------------------------------------- keys and values, by TMA
-        uint32_t it = 0;
+        uint32_t nk = 0, nv = 0;
         for (uint32_t seg = 0; ok && record(seg, r); ++seg) {
             const int32_t *table = p.page_table + size_t(r.b) * p.max_pages;
             const int pages = (r.len + (1 << p.page_shift) - 1) >> p.page_shift;
             int window = (r.t0 * N) >> p.page_shift;         // 32 entries of the table, one a lane, and the 32 behind them
             auto entries = [&](int first) { return r.t0 < r.ct && first + lane < pages ? table[first + lane] : 0; };
             int ids = entries(window), next = entries(window + 32);
+            const int tiles = r.t1 - r.t0;
+            int mine = 0, last = 0;                          // this lane's page of the tile, and of the tile before it
 #pragma unroll 1
-            for (int t = r.t0; t < r.t1 && ok; ++t) {
-                const int valid = valid_of(r, t);
-                const bool draft = t >= r.ct;
-                const int rows = draft ? 16 : box_rows, boxes = (valid + rows - 1) / rows;
-                int y = 0, z = 0;                            // this lane's box: rows into its page, the page and head
-                if (draft) {
-                    y = r.hk;
-                    z = r.l * p.T + r.base + (t - r.ct) * N + lane * 16;
-                } else {
-                    const int at = t * N + lane * rows, page = at >> p.page_shift, first = (t * N) >> p.page_shift;
+            for (int i = 0; i <= tiles && ok; ++i) {
+                const int t = r.t0 + i;
+                last = mine;
+                if (i < tiles && t < r.ct) {
+                    const int page = (t * N + lane * box_rows) >> p.page_shift, first = (t * N) >> p.page_shift;
                     if (first >= window + 32) {
                         window = first;
                         ids = next;
                         next = entries(window + 32);
                     }
-                    int id = __shfl_sync(0xffffffffu, ids, (page - window) & 31);
-                    if (lane < boxes && (id < 0 || id >= p.n_pages)) {
-                        id = 0;                              // read what is there, and leave the unit's outputs alone
+                    mine = __shfl_sync(0xffffffffu, ids, (page - window) & 31);
+                    if (lane * box_rows < valid_of(r, t) && (mine < 0 || mine >= p.n_pages)) {
+                        mine = 0;                            // read what is there, and leave the unit's outputs alone
                         page_bad[seg % kFlagRing] = int(seg) + 1;
                         atomicOr(p.status, SPECA_STATUS_BAD_PAGE);
                     }
-                    y = at & ((1 << p.page_shift) - 1);
-                    z = (r.l * p.n_pages + id) * p.HK + r.hk;
                 }
-                __syncwarp();
+                // keys of this tile, then values of the one before
 #pragma unroll
-                for (int kv = 0; kv < 2; ++kv, ++it) {
-                    const int s = it % SLOTS;
-                    if (!(ok = wait_fast(bar(C::kEmpty + s), ((it / SLOTS) & 1) ^ 1, abort_flag))) break;
-                    const uint32_t full = bar((kv == 1 && to_mend(r, t) ? C::kRaw : C::kFull) + s);
-                    if (lane == 0) mbar_arrive_expect_tx(full, uint32_t(boxes) * rows * (D * 2));
-                    __syncwarp();
-                    if (lane < boxes) {
-                        const CUtensorMap *map = draft ? (kv ? &vd_map : &kd_map) : (kv ? &v_map : &k_map);
-#pragma unroll
-                        for (int c = 0; c < D / 64; ++c)
-                            tma_load_3d(sbase + C::OffRing + s * C::TILE + c * (N * 128) + lane * rows * 128, map, c * 64, y, z, full);
+                for (int kv = 0; kv < 2; ++kv) {
+                    const int tt = t - kv;
+                    if (kv ? i == 0 : i == tiles) continue;
+                    const int n = kv ? nv : nk, s = kv ? n % VS : n % KS, round = kv ? n / VS : n / KS;
+                    if (!(ok = wait_fast(bar((kv ? C::kVEmpty : C::kKEmpty) + s), (round & 1) ^ 1, abort_flag))) break;
+                    (kv ? nv : nk) = n + 1;
+                    const int valid = valid_of(r, tt);
+                    const uint32_t full = bar((kv == 0 ? C::kKFull : to_mend(r, tt) ? C::kVRaw : C::kVFull) + s);
+                    const uint32_t dst = sbase + C::OffRing + (kv ? KS + s : s) * C::TILE;
+                    if (tt >= r.ct) {
+                        const int boxes = (valid + 7) / 8, row = r.l * p.T + r.base + (tt - r.ct) * N;
+                        if (lead) mbar_arrive_expect_tx(full, uint32_t(boxes) * (8 * D * 2));
+                        __syncwarp();
+#pragma unroll 1
+                        for (int j = 0; j < boxes; ++j)
+                            tma_load_4d(dst + j * (8 * D * 2), kv ? &vd_map : &kd_map, 0, row + 8 * j, 0, r.hk, full, lead);
+                    } else {
+                        const int boxes = (valid + box_rows - 1) / box_rows, group = ((tt * N) & ((1 << p.page_shift) - 1)) >> 3;
+                        if (lead) mbar_arrive_expect_tx(full, uint32_t(boxes) * box_rows * (D * 2));
+                        __syncwarp();
+#pragma unroll 1
+                        for (int j = 0; j < boxes; ++j) {
+                            const int id = __shfl_sync(0xffffffffu, kv ? last : mine, j);
+                            tma_load_5d(dst + j * box_rows * (D * 2), kv ? &v_map : &k_map, 0, 0, 0, group, (r.l * p.n_pages + id) * p.HK + r.hk, full, lead);
+                        }
                     }
-                    __syncwarp();
                 }
             }
         }
     } else if (warp == SOFT + 1) {
-        // ------------------------------------------------------------------------------- products
-        const uint32_t id_s = make_idesc_bf16(N), id_o = make_idesc_bf16(D) | (1u << 16);      // (B of the second is MN-major)
-        uint32_t tiles = 0, p_count[2] = {0, 0};
+        // ------------------------------------------------------------------------------- scores
+        const uint32_t id_s = make_idesc_bf16(N);
+        uint32_t loads = 0, phase = 0;                       // tiles of the segments before; next parities
         for (uint32_t seg = 0; ok && record(seg, r); ++seg) {
             const bool two = LANES == 2 && r.rows > 128;     // two row tiles over the same keys
-            const int items = (r.t1 - r.t0) << (two ? 1 : 0);
+            const int tiles = r.t1 - r.t0, items = tiles << (two ? 1 : 0);
             if (!(ok = wait_fast(bar(C::kQFull), seg & 1, abort_flag))) break;
             tc_fence_after();
-            auto scores = [&](int i) -> bool {
-                const uint32_t kt = 2 * (tiles + (two ? i >> 1 : i)), s = kt % SLOTS;
-                const int buf = i & 1;
-                if (!two || buf == 0) {
-                    if (!wait_fast(bar(C::kFull + s), (kt / SLOTS) & 1, abort_flag)) return false;
-                }
-                // the weights of two items ago, in the same columns, have been used
-                if (i >= 2 && !wait_fast(bar(C::kODone + buf), (p_count[buf] - 1) & 1, abort_flag)) return false;
+#pragma unroll 1
+            for (int i = 0; i < items; ++i) {
+                const uint32_t kt = loads + (two ? i >> 1 : i), s = kt % KS;
+                const int buf = buffer(i);
+                if ((!two || !(i & 1)) && !(ok = wait_fast(bar(C::kKFull + s), (kt / KS) & 1, abort_flag))) break;
+                // the weights that were in the same columns have been used
+                if (i >= BUFS && !(ok = wait_fast(bar(C::kODone + buf), ((phase >> buf) & 1) ^ 1, abort_flag))) break;
+                phase ^= 1u << buf;
                 tc_fence_after();
-                const uint32_t qa = sbase + C::OffQ + (two ? buf * C::Q_BYTES : 0), ka = sbase + C::OffRing + s * C::TILE;
+                const uint64_t qd = make_desc(sbase + C::OffQ + (two ? (i & 1) * C::Q_BYTES : 0)), kd = make_desc_k(sbase + C::OffRing + s * C::TILE, 16 * D);
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k)
-                    mma_bf16(tmem + buf * N, make_desc(qa + (k >> 2) * (128 * 128) + (k & 3) * 32),
-                             make_desc(ka + (k >> 2) * (N * 128) + (k & 3) * 32), id_s, k != 0, lead);
+                    mma_bf16(tmem + buf * N, qd + uint64_t(((k >> 2) * (128 * 128) + (k & 3) * 32) >> 4),
+                             kd + uint64_t(((k >> 2) * 1024 + (k & 3) * 32) >> 4), id_s, k != 0, lead);
                 mma_commit(bar(C::kSFull + buf), lead);
-                if (!two || buf == 1) mma_commit(bar(C::kEmpty + s), lead);
-                return true;
-            };
-            if (!(ok = scores(0))) break;
+                if (!two || (i & 1)) mma_commit(bar(C::kKEmpty + s), lead);
+            }
+            loads += tiles;
+        }
+    } else if (warp == SOFT + 2) {
+        // ------------------------------------------------------------------------------- products with V
+        const uint32_t id_o = make_idesc_bf16(D) | (1u << 16);   // (B is MN-major)
+        uint32_t loads = 0, phase = 0;
+        for (uint32_t seg = 0; ok && record(seg, r); ++seg) {
+            const bool two = LANES == 2 && r.rows > 128;
+            const int tiles = r.t1 - r.t0, items = tiles << (two ? 1 : 0);
 #pragma unroll 1
-            for (int i = 0; i < items && ok; ++i) {
-                if (i + 1 < items && !(ok = scores(i + 1))) break;
-                const int buf = i & 1, t = r.t0 + (two ? i >> 1 : i), valid = valid_of(r, t);
-                const uint32_t vt = 2 * (tiles + (two ? i >> 1 : i)) + 1, s = vt % SLOTS;
-                if ((!two || buf == 0) && !(ok = wait_fast(bar(C::kFull + s), (vt / SLOTS) & 1, abort_flag))) break;
-                if (!(ok = wait_fast(bar(C::kPReady + buf), p_count[buf] & 1, abort_flag))) break;
-                ++p_count[buf];
+            for (int i = 0; i < items; ++i) {
+                const int buf = buffer(i), ti = two ? i >> 1 : i, valid = valid_of(r, r.t0 + ti);
+                const uint32_t vt = loads + ti, s = vt % VS;
+                if ((!two || !(i & 1)) && !(ok = wait_fast(bar(C::kVFull + s), (vt / VS) & 1, abort_flag))) break;
+                if (!(ok = wait_fast(bar(C::kPReady + buf), (phase >> buf) & 1, abort_flag))) break;
+                phase ^= 1u << buf;
                 tc_fence_after();
-                const int oc = LANES == 2 ? kOCol + buf * D : kOCol, steps = (valid + 15) >> 4;
-                const bool fresh = LANES == 2 ? i < 2 : i == 0;
-                const uint64_t vd = make_desc_mn(sbase + C::OffRing + s * C::TILE, N * 128);
+                const int oc = LANES == 2 ? kOCol + (i & 1) * D : kOCol, steps = (valid + 15) >> 4;
+                const uint64_t vd = make_desc_mn(sbase + C::OffRing + (KS + s) * C::TILE, 16 * D);
 #pragma unroll
                 for (int k = 0; k < N / 16; ++k)
                     if (k < steps)
-                        mma_bf16_ts(tmem + oc, tmem + buf * N + 8 * k, vd + uint64_t(k * (16 * 128 >> 4)), id_o, !(fresh && k == 0), lead);
+                        mma_bf16_ts(tmem + oc, tmem + buf * N + 8 * k, vd + uint64_t(k * (2 * 16 * D >> 4)), id_o, !(i < LANES && k == 0), lead);
                 mma_commit(bar(C::kODone + buf), lead);
-                if (!two || buf == 1) mma_commit(bar(C::kEmpty + s), lead);
+                if (!two || (i & 1)) mma_commit(bar(C::kVEmpty + s), lead);
             }
-            tiles += r.t1 - r.t0;
+            loads += tiles;
         }
-    } else if (warp == SOFT + 2) {
+    } else if (warp == SOFT + 3) {
         // ------------------------------------------------------------------------------- mending of V
         // A weight of zero does not take a value that is not finite out of a product: rows past the end of a tile's keys (what
         // was there before, another sequence's, or never written) are set to zero, and so are draft values that are not finite,
         // which only some rows attend; those get them back at the end.
-        uint32_t tiles = 0, phase = 0;                       // phase: a bit a slot
-        for (uint32_t seg = 0; ok && record(seg, r); ++seg) {
+        uint32_t loads = 0, phase = 0;                       // phase: a bit a slot
+        for (uint32_t seg = 0; ok && record(seg, r); loads += r.t1 - r.t0, ++seg) {
 #pragma unroll 1
-            for (int t = r.t0; t < r.t1; ++t, ++tiles) {
+            for (int t = r.t0; t < r.t1; ++t) {
                 if (!to_mend(r, t)) continue;
                 const int valid = valid_of(r, t);
                 const bool draft = t >= r.ct;
-                const uint32_t s = (2 * tiles + 1) % SLOTS;
-                if (!(ok = wait_fast(bar(C::kRaw + s), (phase >> s) & 1, abort_flag))) break;
+                const uint32_t s = (loads + (t - r.t0)) % VS;
+                if (!(ok = wait_fast(bar(C::kVRaw + s), (phase >> s) & 1, abort_flag))) break;
                 phase ^= 1u << s;
-                uint8_t *v = smem + C::OffRing + s * C::TILE;
+                uint8_t *v = smem + C::OffRing + (KS + s) * C::TILE;
                 const int end = (valid + 15) & ~15;
                 for (int i = valid * (D / 8) + lane; i < end * (D / 8); i += 32) {
                     const int row = i / (D / 8), c = i % (D / 8);
-                    *reinterpret_cast<uint4 *>(v + (c >> 3) * (N * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+                    *reinterpret_cast<uint4 *>(v + tile_offset<D>(row, c)) = make_uint4(0u, 0u, 0u, 0u);
                 }
                 if (draft) {
                     bool bad = false;
 #pragma unroll 4
                     for (int i = lane; i < valid * (D / 8); i += 32) {
                         const int row = i / (D / 8), c = i % (D / 8);
-                        uint4 *at = reinterpret_cast<uint4 *>(v + (c >> 3) * (N * 128) + row * 128 + (c & 7) * 16);
+                        uint4 *at = reinterpret_cast<uint4 *>(v + tile_offset<D>(row, c));
                         const uint4 x = *at;
                         if (not_finite(x.x) || not_finite(x.y) || not_finite(x.z) || not_finite(x.w)) {
                             uint32_t w[4] = {x.x, x.y, x.z, x.w};
@@ -440,10 +531,10 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
                 }
                 fence_proxy_async();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(C::kFull + s));
+                if (lane == 0) mbar_arrive(bar(C::kVFull + s));
             }
         }
-    } else if (warp == SOFT + 3) {
+    } else if (warp == SOFT + 4) {
         // ------------------------------------------------------------------------------- schedule
         Join join{0, 0, 0, 0, 0, 0, 0, 0};
         uint32_t seg = 0;
@@ -504,7 +595,7 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
         const int wg = warp >> 2, quad = warp & 3, trow = quad * 32 + lane;      // lane of TMEM: row of this group's tile
         const uint32_t tq = tmem + (uint32_t(quad * 32) << 16);
         const float c2 = p.scale * 1.4426950408889634f;
-        uint32_t syncs = 0, cnt[2] = {0, 0};                 // items of each buffer in earlier segments
+        uint32_t syncs = 0, phase = 0;
         int16_t *par = reinterpret_cast<int16_t *>(smem + C::OffPar);
         auto sync = [&]() -> bool {
             __syncwarp();
@@ -514,7 +605,7 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
         for (uint32_t seg = 0; ok && record(seg, r); ++seg) {
             const bool two = LANES == 2 && r.rows > 128;
             const int tiles = r.t1 - r.t0;
-            const int n_buf[2] = {two ? tiles : (tiles + 1) / 2, two ? tiles : tiles / 2};
+            const int all = tiles << (two ? 1 : 0);          // items of both groups
             // everyone is through with the last segment: its queries, its parents, its sums
             if (!(ok = sync())) break;
             if (threadIdx.x == 0) topo_bad[(seg & 1) ^ 1] = 0;
@@ -548,24 +639,20 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
             const bool live = (two ? wg * 128 : 0) + quad * 32 < r.rows;     // the warp has rows
             const int at = r.row0 + (row < r.rows ? row : 0), node = at / group, g = at - node * group;
             float m = -INFINITY, l = 0.f;
-            const int items = LANES == 2 ? n_buf[wg] : tiles;
+            const int mine = LANES == 2 ? (all + 1 - wg) / 2 : all;          // items of this group
+            uint32_t uses = phase;                           // parities that its own items have turned
 #pragma unroll 1
-            for (int i = 0; i < items; ++i) {
-                // (one group has all items, alternately in the two buffers; two groups have a buffer each)
-                const int buf = LANES == 2 ? wg : i & 1;
-                const uint32_t k = LANES == 2 ? cnt[wg] + i : cnt[i & 1] + (i >> 1);         // items of that buffer so far
-                const int t = r.t0 + (LANES == 2 ? (two ? i : 2 * i + wg) : i);
-                if (!(ok = wait_fast(bar(C::kSFull + buf), k & 1, abort_flag))) break;
+            for (int i = 0; i < mine; ++i) {
+                const int item = LANES == 2 ? 2 * i + wg : i, buf = buffer(item), t = r.t0 + (two ? i : item);
+                if (!(ok = wait_fast(bar(C::kSFull + buf), (uses >> buf) & 1, abort_flag))) break;
+                uses ^= 1u << buf;
                 tc_fence_after();
                 if (live) {
                     const uint32_t ta = tq + buf * N;
-                    float s[N];
-#pragma unroll
-                    for (int c = 0; c < N / 32; ++c) tmem_ld32(ta + 32 * c, s + 32 * c);
-                    tmem_ld_wait();
                     const int valid = valid_of(r, t);
-                    if (t >= r.ct || valid < N) {
-                        uint32_t mask[N / 32];
+                    const bool masked = t >= r.ct || valid < N;
+                    uint32_t mask[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
+                    if (masked) {
                         const int first = (t - r.ct) * N;    // first node of a draft tile
                         if (t < r.ct || p.parent == nullptr) {
                             const int upto = t < r.ct ? valid : node + 1 - first;
@@ -583,20 +670,39 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
                                 for (int w = 0; w < N / 32; ++w) mask[w] |= (x >> 5) == w ? 1u << (x & 31) : 0u;
                             }
                         }
-#pragma unroll
-                        for (int c = 0; c < N; ++c)
-                            if (!(mask[c >> 5] >> (c & 31) & 1u)) s[c] = -INFINITY;
                     }
-                    float top4[4] = {s[0], s[1], s[2], s[3]};
+                    // Scores are read twice, for the maximum and for the weights, 32 at a time: these loops and what stands around
+                    // them have to stay in the instruction cache together (unrolled over the tile, the end of every segment
+                    // was fetched anew, at 6000 to 11000 cycles for a few hundred instructions).
+                    float s[32];
+                    auto load = [&](int c) {
+                        tmem_ld32(ta + 32 * c, s);
+                        tmem_ld_wait();
+                        if (masked) {
+                            const uint32_t w = c == 0 ? mask[0] : c == 1 ? mask[1] : c == 2 ? mask[2] : mask[3];
 #pragma unroll
-                    for (int c = 4; c < N; ++c) top4[c & 3] = fmaxf(top4[c & 3], s[c]);
-                    const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
+                            for (int e = 0; e < 32; ++e)
+                                if (!(w >> e & 1u)) s[e] = -INFINITY;
+                        }
+                    };
+                    float top = -INFINITY, other = -INFINITY;
+#pragma unroll 1
+                    for (int c = 0; c < N / 32; ++c) {
+                        load(c);
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4) {
+                            top = max3(top, s[e], s[e + 1]);
+                            other = max3(other, s[e + 2], s[e + 3]);
+                        }
+                    }
+                    top = fmaxf(top, other);
                     if (i == 0) m = top;
-                    else if (__any_sync(0xffffffffu, (top - m) * c2 > kSlack || (m == -INFINITY && top > m))) {
-                        // the last item's product must have been added before O is scaled
-                        const int pb = LANES == 2 ? wg : (i - 1) & 1;
-                        const uint32_t pk = LANES == 2 ? k - 1 : cnt[pb] + ((i - 1) >> 1);
-                        if (!(ok = wait_fast(bar(C::kODone + pb), pk & 1, abort_flag))) break;
+                    // (rows past the unit's last hold whatever was there: they have no say)
+                    else if (__any_sync(0xffffffffu, row < r.rows && ((top - m) * c2 > kSlack || (m == -INFINITY && top > m)))) {
+                        // the last item's product must have been added before O is scaled (where that item had this
+                        // buffer too, its parity is two turns old)
+                        const int pb = buffer(item - LANES);
+                        if (!(ok = wait_fast(bar(C::kODone + pb), ((uses >> pb) & 1) ^ (pb != buf), abort_flag))) break;
                         tc_fence_after();
                         const float now = fmaxf(m, top);
                         // (before its first key a row's sums are zero, in whatever scale)
@@ -605,35 +711,39 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
                         l *= f;
                         const uint32_t to = tq + kOCol + (LANES == 2 ? wg * D : 0);
 #pragma unroll 1
-                        for (int c = 0; c < D; c += 32) {
-                            float o[32];
-                            tmem_ld32(to + c, o);
-                            tmem_ld_wait();
+                        for (int c = 0; c < D; c += 16) {
+                            float o[16];
                             uint32_t x[16];
+                            tmem_ld16(to + c, o);
+                            tmem_ld_wait();
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                                for (int e = 0; e < 16; ++e) x[e] = __float_as_uint(o[16 * h + e] * f);
-                                tmem_st16(to + c + 16 * h, x);
-                            }
+                            for (int e = 0; e < 16; ++e) x[e] = __float_as_uint(o[e] * f);
+                            tmem_st16(to + c, x);
                         }
                         tmem_st_wait();
                     }
                     const float mc = m == -INFINITY ? 0.f : m * c2;
-                    float add[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
+                    const uint64_t scale2 = pair2(c2, c2), shift2 = pair2(-mc, -mc);
+                    uint64_t add[2] = {0u, 0u};
+#pragma unroll 1
                     for (int c = 0; c < N / 32; ++c) {
+                        load(c);
                         uint32_t x[16];
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
-                            const float a = exp2_approx(fmaf(s[32 * c + 2 * e], c2, -mc)), b = exp2_approx(fmaf(s[32 * c + 2 * e + 1], c2, -mc));
-                            add[(2 * e) & 3] += a;
-                            add[(2 * e + 1) & 3] += b;
+                            float a, b;
+                            unpair2(fma2(pair2(s[2 * e], s[2 * e + 1]), scale2, shift2), a, b);
+                            a = exp2_approx(a);
+                            b = exp2_approx(b);
+                            add[e & 1] = add2(add[e & 1], pair2(a, b));
                             x[e] = pack_bf16(a, b);
                         }
-                        tmem_st16(ta + 16 * c, x);
+                        tmem_st16(ta + 16 * c, x);           // (over scores that have been read)
                     }
-                    l += (add[0] + add[1]) + (add[2] + add[3]);
+                    float a0, a1, a2, a3;
+                    unpair2(add[0], a0, a1);
+                    unpair2(add[1], a2, a3);
+                    l += (a0 + a1) + (a2 + a3);
                     tmem_st_wait();
                     tc_fence_before();
                 }
@@ -642,79 +752,82 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
             }
             if (!ok) break;
 
-            // ---- end of the segment.  Sums of even and odd tiles: both groups read both, half of the columns each.
+            // ---- end of the segment: this group's last product covers those before it
             const bool merge = LANES == 2 && !two;
+            if (mine > 0) {
+                const int last = buffer(LANES == 2 ? 2 * (mine - 1) + wg : mine - 1);
+                if (!(ok = wait_fast(bar(C::kODone + last), ((uses >> last) & 1) ^ 1, abort_flag))) break;
+            }
+#pragma unroll
+            for (int b = 0; b < BUFS; ++b) phase ^= uint32_t((all + BUFS - 1 - b) / BUFS & 1) << b;      // items of all groups in buffer b
+            tc_fence_after();
             float f0 = 1.f, f1 = 0.f, mm = m, ll = l;
             if (merge) {
-                float2 *ex = reinterpret_cast<float2 *>(smem + C::OffQ + C::Q_BYTES);        // (the second row tile's queries: there are none)
-                ex[wg * 128 + trow] = make_float2(m, l);
+                // Sums of even and odd tiles: both groups read both, half of the columns each.  Maxima and sums of weights go through
+                // the columns of the group's last weights.
+                tmem_st2(tq + wg * N, m, l);
+                tmem_st_wait();
+                tc_fence_before();
                 if (!(ok = sync())) break;
-                const float2 a = ex[trow], b = ex[128 + trow];
+                tc_fence_after();
+                float2 a, b;
+                tmem_ld2(tq, a);
+                tmem_ld2(tq + N, b);
+                tmem_ld_wait();
                 mm = fmaxf(a.x, b.x);
                 const float base = mm == -INFINITY ? 0.f : mm;
                 f0 = a.x == mm ? 1.f : exp2_approx((a.x - base) * c2);
                 f1 = b.x == mm ? 1.f : exp2_approx((b.x - base) * c2);
                 // (a maximum that is not a number belongs to sums that are not either)
-                ll = a.y * f0 + (n_buf[1] > 0 ? b.y * f1 : 0.f);
+                ll = a.y * f0 + (all > 1 ? b.y * f1 : 0.f);
             }
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const bool need = merge ? n_buf[b] > 0 : LANES == 2 ? b == wg : b == ((tiles - 1) & 1);
-                if (need && ok) ok = wait_fast(bar(C::kODone + b), (cnt[b] + n_buf[b] - 1) & 1, abort_flag);
-            }
-            if (!ok) break;
-            tc_fence_after();
             const bool bad = topo_bad[seg & 1] != 0 && p.parent != nullptr && r.t1 > r.ct;
             const bool skip = bad || page_bad[seg % kFlagRing] == int(seg) + 1;
             const bool mend = value_bad[seg % kFlagRing] == int(seg) + 1;
             if (live) {
                 const uint32_t o0 = tq + kOCol + (LANES == 2 && two ? wg * D : 0), o1 = tq + kOCol + D;
-                const bool both = merge && n_buf[1] > 0;
+                const bool both = merge && all > 1;
                 const int c_lo = merge ? wg * (D / 2) : 0, c_hi = merge ? c_lo + D / 2 : D;
                 const float inv = 1.f / ll;
                 float *sums = r.slot >= 0 ? slot_sums(plan, cta, r.slot) : nullptr;
+                __nv_bfloat16 *out = p.o + ((size_t(r.l) * p.T + r.base + node) * p.H + r.hk * group + g) * D;
+                const bool write = row < r.rows && !skip;
+                if (sums == nullptr) { f0 *= inv; f1 *= inv; }
 #pragma unroll 1
-                for (int c = c_lo; c < c_hi; c += 32) {
-                    float o[32];
-                    tmem_ld32(o0 + c, o);
+                for (int c = c_lo; c < c_hi; c += 16) {
+                    float o[16], x[16];
+                    tmem_ld16(o0 + c, o);
+                    if (both) tmem_ld16(o1 + c, x);
                     tmem_ld_wait();
-                    if (merge) {
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] *= f0;
-                        if (both) {
-                            float x[32];
-                            tmem_ld32(o1 + c, x);
-                            tmem_ld_wait();
+                    for (int e = 0; e < 16; ++e) o[e] = both ? fmaf(x[e], f1, o[e] * f0) : o[e] * f0;
+                    if (!write) continue;
+                    if (sums == nullptr) {
+                        uint4 *to = reinterpret_cast<uint4 *>(out + c);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) o[e] = fmaf(x[e], f1, o[e]);
-                        }
+                        for (int e = 0; e < 2; ++e)
+                            to[e] = make_uint4(pack_bf16(o[8 * e], o[8 * e + 1]), pack_bf16(o[8 * e + 2], o[8 * e + 3]),
+                                               pack_bf16(o[8 * e + 4], o[8 * e + 5]), pack_bf16(o[8 * e + 6], o[8 * e + 7]));
+                    } else {
+                        float4 *to = reinterpret_cast<float4 *>(sums + size_t(row) * D + c);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) to[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
                     }
-                    if (mend) {
-                        // draft values that are not finite, of the nodes that this row attends
-                        const int lo = r.t0 < r.ct ? 0 : (r.t0 - r.ct) * N, hi = (r.t1 - r.ct) * N;
-                        for (int a = node; a >= lo; a = p.parent != nullptr ? int(par[a]) : a - 1)
-                            if (a < hi) {
-                                const __nv_bfloat16 *v = p.v + ((size_t(r.l) * p.T + r.base + a) * p.HK + r.hk) * D + c;
-#pragma unroll
-                                for (int e = 0; e < 32; ++e) {
-                                    const float x = __bfloat162float(v[e]);
-                                    if (!isfinite(x)) o[e] += x;
-                                }
+                }
+                if (mend && write) {
+                    // draft values that are not finite, of the nodes that this row attends, go on top of what was written
+                    const int lo = r.t0 < r.ct ? 0 : (r.t0 - r.ct) * N, hi = (r.t1 - r.ct) * N;
+                    for (int a = node; a >= lo; a = p.parent != nullptr ? int(par[a]) : a - 1)
+                        if (a < hi) {
+                            const __nv_bfloat16 *v = p.v + ((size_t(r.l) * p.T + r.base + a) * p.HK + r.hk) * D;
+#pragma unroll 1
+                            for (int c = c_lo; c < c_hi; ++c) {
+                                const float x = __bfloat162float(v[c]);
+                                if (isfinite(x)) continue;
+                                if (sums == nullptr) out[c] = __float2bfloat16_rn(__bfloat162float(out[c]) + x);
+                                else sums[size_t(row) * D + c] += x;
                             }
-                    }
-                    if (row < r.rows && !skip) {
-                        if (sums == nullptr) {
-                            uint4 *to = reinterpret_cast<uint4 *>(p.o + ((size_t(r.l) * p.T + r.base + node) * p.H + r.hk * group + g) * D + c);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                to[e] = make_uint4(pack_bf16(o[8 * e] * inv, o[8 * e + 1] * inv), pack_bf16(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
-                                                   pack_bf16(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_bf16(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
-                        } else {
-                            float4 *to = reinterpret_cast<float4 *>(sums + size_t(row) * D + c);
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) to[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
                         }
-                    }
                 }
                 if (sums != nullptr) {
                     float *tail = sums + size_t(plan.rows_cap) * D;
@@ -723,13 +836,11 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
                 }
             }
             tc_fence_before();
-            cnt[0] += n_buf[0];
-            cnt[1] += n_buf[1];
         }
     }
 
-    if (warp == SOFT + 1) {
-        // everything this warp issued must have completed before TMEM is released
+    if (warp == SOFT + 1 || warp == SOFT + 2) {
+        // everything these warps issued must have completed before TMEM is released
         mma_commit(bar(C::kDrain), lead);
         mbar_wait(bar(C::kDrain), 0, abort_flag);
     }
@@ -818,15 +929,17 @@ template <int D> int launch_width(const AttnParams &p, cudaStream_t st)
     }
     const int page = 1 << p.page_shift, box_rows = page < C::N ? page : C::N;
     CUtensorMap maps[4];
-    const cuuint32_t es[3] = {1, 1, 1};
+    const cuuint32_t es[5] = {1, 1, 1, 1, 1};
     for (int i = 0; i < 4; ++i) {
         const bool cache = i < 2;
         const void *base = i == 0 ? p.k_cache : i == 1 ? p.v_cache : i == 2 ? p.k : p.v;
-        const cuuint64_t dim[3] = {cuuint64_t(D), cuuint64_t(cache ? page : p.HK),
-                                   cache ? cuuint64_t(p.L) * p.n_pages * p.HK : cuuint64_t(p.L) * p.T};
-        const cuuint64_t stride[2] = {cuuint64_t(D) * 2, dim[1] * D * 2};
-        const cuuint32_t box[3] = {64, cuuint32_t(cache ? box_rows : 1), cuuint32_t(cache ? 1 : 16)};
-        if (encode(&maps[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dim, stride, box, es,
+        // 64 columns, eight rows, blocks of columns; of the cache groups of eight rows and (layer, page, head) besides, of the
+        // draft rows of all layers in place of the eight, and the head
+        const cuuint64_t row = cuuint64_t(D) * 2 * (cache ? 1 : p.HK);
+        const cuuint64_t dim[5] = {64, cache ? 8u : cuuint64_t(p.L) * p.T, D / 64, cuuint64_t(cache ? page / 8 : p.HK), cuuint64_t(p.L) * p.n_pages * p.HK};
+        const cuuint64_t stride[4] = {row, 128, cache ? 8 * row : cuuint64_t(D) * 2, cuuint64_t(page) * D * 2};
+        const cuuint32_t box[5] = {64, 8, D / 64, cuuint32_t(cache ? box_rows / 8 : 1), 1};
+        if (encode(&maps[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, cache ? 5 : 4, const_cast<void *>(base), dim, stride, box, es,
                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
             return int(cudaErrorInvalidValue);
