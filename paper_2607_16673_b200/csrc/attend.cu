@@ -253,15 +253,29 @@ template <int D> __device__ __forceinline__ long unit_tiles(const Seq &s, int gr
 {
     return s.ct + (nodes_seen<Cfg<D>::MT>(s.n, group, m) + Cfg<D>::N - 1) / Cfg<D>::N;
 }
+// Cost of a unit, in tiles of 128 rows: its own (twice as many where two row tiles share the keys) and what begins and ends it,
+// queries in, sums out, the pipeline filled and drained (8000 to 17000 cycles, a tile 2500 to 3500).  Pieces are equal in this
+// measure: with tiles alone counted, CTAs that got many short sequences took up to twice as long as the others.
+template <int D> struct Cost {
+    static constexpr int kEnds = D == 256 ? 5 : 3;
+};
+template <int D> __device__ __forceinline__ int tile_cost(const Seq &s, int group, int m)
+{
+    return Cfg<D>::LANES == 2 && s.n * group - m * Cfg<D>::MT > 128 ? 2 : 1;
+}
+template <int D> __device__ __forceinline__ long unit_cost(const Seq &s, int group, int m)
+{
+    return unit_tiles<D>(s, group, m) * tile_cost<D>(s, group, m) + Cost<D>::kEnds;
+}
 template <int D> __device__ __forceinline__ int row_tiles(const Seq &s, int group)
 {
     return (s.n * group + Cfg<D>::MT - 1) / Cfg<D>::MT;     // (at most 8192 nodes and 65536 heads)
 }
-// tiles of one layer and key head
-template <int D> __device__ __forceinline__ long head_tiles(const Seq &s, int group)
+// cost of one layer and key head
+template <int D> __device__ __forceinline__ long head_cost(const Seq &s, int group)
 {
     long sum = 0;
-    for (int m = 0; m < row_tiles<D>(s, group); ++m) sum += unit_tiles<D>(s, group, m);
+    for (int m = 0; m < row_tiles<D>(s, group); ++m) sum += unit_cost<D>(s, group, m);
     return sum;
 }
 
@@ -306,7 +320,7 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
     }
     if (warp == SOFT + 1) tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_slot)), kTmemCols);
 
-    // ---- tiles of the whole list, and where this CTA's piece begins: every thread has some consecutive sequences
+    // ---- cost of the whole list, and where this CTA's piece begins: every thread has some consecutive sequences
     long mine = 0, before = 0, total = 0;
     const int per_thread = (p.B + C::THREADS - 1) / C::THREADS;
     const int b_lo = min(p.B, int(threadIdx.x) * per_thread), b_hi = min(p.B, b_lo + per_thread);
@@ -314,7 +328,7 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
     for (int b = b_lo; b < b_hi; ++b) {
         const Seq s = sequence<N>(p, b);
         if (s.fault && cta == 0) atomicOr(p.status, s.fault);
-        mine += heads * head_tiles<D>(s, group);
+        mine += heads * head_cost<D>(s, group);
     }
     long incl = mine;
 #pragma unroll
@@ -332,13 +346,15 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
         total += sums[w];
     }
     before += incl - mine;
-    const long per = total / grid, extra = total % grid;
-    const long begin = cta * per + min(long(cta), extra), count = per + (cta < extra ? 1 : 0);
+    // (a piece is at least one tile long, so that every CTA between a unit's first and last has some of it)
+    const int pieces = int(min(long(grid), max(1L, total / (plan.rows_cap > 128 ? 2 : 1))));
+    const long per = total / pieces, extra = total % pieces;
+    const long begin = cta * per + min(long(cta), extra), count = cta < pieces ? per + (cta < extra ? 1 : 0) : 0;
     if (count > 0 && begin >= before && begin < before + mine) {
         long rem = begin - before;
         int b = b_lo;
         for (;; ++b) {
-            const long t = heads * head_tiles<D>(sequence<N>(p, b), group);
+            const long t = heads * head_cost<D>(sequence<N>(p, b), group);
             if (rem < t) break;
             rem -= t;
         }
@@ -368,7 +384,9 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
     };
     // (A barrier has two parities: whoever waits on one waits for all its phases in turn.  So keys and values have rings of
     // their own, and values that are looked over before they are used land on a barrier of their own.)
-    auto to_mend = [&](const Rec &r, int t) { return t >= r.ct || (valid_of(r, t) & 15) != 0; };
+    // (a chain's draft keys below the first of the unit's nodes: every row attends them all)
+    auto all_seen = [&](const Rec &r, int t) { return t < r.ct || (p.parent == nullptr && (t - r.ct + 1) * N <= r.row0 / group + 1); };
+    auto to_mend = [&](const Rec &r, int t) { return (valid_of(r, t) & 15) != 0 || !all_seen(r, t); };
     // Buffer of item i of a segment.  Every use of a buffer is one phase of its three barriers (scores there, weights there,
     // weights used); a role keeps the parity of the next one, a bit a buffer.
     auto buffer = [](int i) { return LANES == 2 ? i & 1 : i % 3; };
@@ -499,7 +517,7 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
             for (int t = r.t0; t < r.t1; ++t) {
                 if (!to_mend(r, t)) continue;
                 const int valid = valid_of(r, t);
-                const bool draft = t >= r.ct;
+                const bool draft = !all_seen(r, t);
                 const uint32_t s = (loads + (t - r.t0)) % VS;
                 if (!(ok = wait_fast(bar(C::kVRaw + s), (phase >> s) & 1, abort_flag))) break;
                 phase ^= 1u << s;
@@ -551,34 +569,40 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
         long left = count;
         if (left > 0) {
             int b = start[0];
-            long rem = (long(start[3]) << 32) | uint32_t(start[2]);
-            long at = begin;                                 // place in the whole list
-            for (; left > 0 && ok; ++b, rem = 0) {
+            long in = (long(start[3]) << 32) | uint32_t(start[2]);       // place in the sequence where the piece begins
+            for (; left > 0 && ok; ++b, in = 0) {
                 const Seq s = sequence<N>(p, b);
-                const long ht = head_tiles<D>(s, group);
-                if (ht == 0) continue;
-                long hd = rem / ht, in = rem % ht;
+                const long hc = head_cost<D>(s, group);
+                if (hc == 0) continue;
                 const int mts = row_tiles<D>(s, group);
-                for (; hd < heads && left > 0 && ok; ++hd, in = 0) {
+                long hd = in / hc;
+                in -= hd * hc;
+                for (; hd < heads && left > 0 && ok; ++hd) {
                     for (int m = 0; m < mts && left > 0 && ok; ++m) {
-                        const long ut = unit_tiles<D>(s, group, m);
-                        if (in >= ut) { in -= ut; continue; }
-                        const long take = min(left, ut - in);
+                        const long uc = unit_cost<D>(s, group, m);
+                        if (in >= uc) { in -= uc; continue; }
+                        // the unit's ends stand before its tiles; a tile is whose piece its beginning is in
+                        const int ut = int(unit_tiles<D>(s, group, m)), w = tile_cost<D>(s, group, m);
+                        auto tile_at = [&](long x) { return int(min(long(ut), max(0L, (x - Cost<D>::kEnds + w - 1) / w))); };
+                        const long take = min(left, uc - in);
                         Rec x{};
-                        x.l = int(hd / p.HK); x.b = b; x.hk = int(hd % p.HK); x.base = s.base; x.n = s.n; x.len = s.len;
-                        x.row0 = m * C::MT;
-                        x.rows = int(min(long(C::MT), long(s.n) * group - x.row0));
-                        x.t0 = int(in); x.t1 = int(in + take); x.ct = s.ct;
-                        x.nodes = nodes_seen<C::MT>(s.n, group, m);
-                        x.slot = take == ut ? -1 : in == 0 ? 1 : 0;
-                        if (x.slot == 1) {
-                            // the unit ends in a later CTA's piece
-                            const long last = at + ut - 1, wide = extra * (per + 1);
-                            const int owner = int(last < wide ? last / (per + 1) : extra + (last - wide) / per);
-                            join = Join{owner - cta + 1, x.l, x.hk, x.base, x.row0, x.rows, 0, 0};
+                        x.t0 = tile_at(in);
+                        x.t1 = tile_at(in + take);
+                        if (x.t1 > x.t0) {
+                            x.l = int(hd / p.HK); x.b = b; x.hk = int(hd % p.HK); x.base = s.base; x.n = s.n; x.len = s.len;
+                            x.row0 = m * C::MT;
+                            x.rows = min(C::MT, s.n * group - x.row0);
+                            x.ct = s.ct;
+                            x.nodes = nodes_seen<C::MT>(s.n, group, m);
+                            x.slot = x.t0 == 0 && x.t1 == ut ? -1 : x.t0 == 0 ? 1 : 0;
+                            if (x.slot == 1) {
+                                // the unit ends in a later CTA's piece: where its last tile begins
+                                const long last = begin + (count - left) - in + Cost<D>::kEnds + long(ut - 1) * w, wide = extra * (per + 1);
+                                const int owner = int(last < wide ? last / (per + 1) : extra + (last - wide) / per);
+                                join = Join{owner - cta + 1, x.l, x.hk, x.base, x.row0, x.rows, 0, 0};
+                            }
+                            put(x);
                         }
-                        put(x);
-                        at += take;
                         left -= take;
                         in = 0;
                     }
@@ -650,7 +674,7 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
                 if (live) {
                     const uint32_t ta = tq + buf * N;
                     const int valid = valid_of(r, t);
-                    const bool masked = t >= r.ct || valid < N;
+                    const bool masked = valid < N || !all_seen(r, t);
                     uint32_t mask[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
                     if (masked) {
                         const int first = (t - r.ct) * N;    // first node of a draft tile
@@ -793,27 +817,53 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
                 __nv_bfloat16 *out = p.o + ((size_t(r.l) * p.T + r.base + node) * p.H + r.hk * group + g) * D;
                 const bool write = row < r.rows && !skip;
                 if (sums == nullptr) { f0 *= inv; f1 *= inv; }
+                // Through shared memory (this group's queries have been used), so that a row is written in whole lines: straight
+                // from the lanes, a row each, a store touched 32 lines, and 128 rows took 9000 cycles.
+                uint8_t *stage = smem + C::OffQ + (LANES == 2 ? wg : 0) * C::Q_BYTES + quad * 4096;
+                const uint64_t out_at = reinterpret_cast<uint64_t>(out);
+                const int rows_here = min(32, r.rows - (row - lane));
 #pragma unroll 1
-                for (int c = c_lo; c < c_hi; c += 16) {
-                    float o[16], x[16];
-                    tmem_ld16(o0 + c, o);
-                    if (both) tmem_ld16(o1 + c, x);
+                for (int c = c_lo; c < c_hi; c += 32) {
+                    float o[32];
+                    tmem_ld32(o0 + c, o);
                     tmem_ld_wait();
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) o[e] = both ? fmaf(x[e], f1, o[e] * f0) : o[e] * f0;
-                    if (!write) continue;
+                    for (int e = 0; e < 32; ++e) o[e] *= f0;
+                    if (both) {
+                        float x[32];
+                        tmem_ld32(o1 + c, x);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = fmaf(x[e], f1, o[e]);
+                    }
+                    if (skip) continue;
+                    __syncwarp();
                     if (sums == nullptr) {
-                        uint4 *to = reinterpret_cast<uint4 *>(out + c);
 #pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            to[e] = make_uint4(pack_bf16(o[8 * e], o[8 * e + 1]), pack_bf16(o[8 * e + 2], o[8 * e + 3]),
-                                               pack_bf16(o[8 * e + 4], o[8 * e + 5]), pack_bf16(o[8 * e + 6], o[8 * e + 7]));
+                        for (int e = 0; e < 4; ++e)
+                            *reinterpret_cast<uint4 *>(stage + lane * 64 + ((e ^ (lane >> 1 & 3)) << 4)) =
+                                make_uint4(pack_bf16(o[8 * e], o[8 * e + 1]), pack_bf16(o[8 * e + 2], o[8 * e + 3]),
+                                           pack_bf16(o[8 * e + 4], o[8 * e + 5]), pack_bf16(o[8 * e + 6], o[8 * e + 7]));
+                        __syncwarp();
+                        for (int i = 0; i < rows_here; i += 8) {
+                            const int rr = i + (lane >> 2);
+                            uint8_t *to = reinterpret_cast<uint8_t *>(__shfl_sync(0xffffffffu, out_at, rr)) + c * 2 + (lane & 3) * 16;
+                            const uint4 x = *reinterpret_cast<const uint4 *>(stage + rr * 64 + (((lane & 3) ^ (rr >> 1 & 3)) << 4));
+                            if (rr < rows_here) *reinterpret_cast<uint4 *>(to) = x;
+                        }
                     } else {
-                        float4 *to = reinterpret_cast<float4 *>(sums + size_t(row) * D + c);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) to[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                        for (int e = 0; e < 8; ++e)
+                            *reinterpret_cast<float4 *>(stage + lane * 128 + ((e ^ (lane & 7)) << 4)) = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                        __syncwarp();
+                        for (int i = 0; i < rows_here; i += 4) {
+                            const int rr = i + (lane >> 3);
+                            const uint4 x = *reinterpret_cast<const uint4 *>(stage + rr * 128 + (((lane & 7) ^ (rr & 7)) << 4));
+                            if (rr < rows_here) *reinterpret_cast<uint4 *>(sums + size_t(row - lane + rr) * D + c + (lane & 7) * 4) = x;
+                        }
                     }
                 }
+                __syncwarp();
                 if (mend && write) {
                     // draft values that are not finite, of the nodes that this row attends, go on top of what was written
                     const int lo = r.t0 < r.ct ? 0 : (r.t0 - r.ct) * N, hi = (r.t1 - r.ct) * N;
