@@ -10,32 +10,31 @@
 // Work: the tiles of all (sequence, layer, key head, row tile) units stand in one list, and every CTA takes an equal piece of
 // it, so the batch's lengths do not matter and a single long context occupies every SM.  A unit cut by the border of two
 // pieces leaves unnormalised sums with their maxima in the workspace, which a second kernel joins in the order of the pieces.
-#include "attn.cuh"
-#include "tc_ptx.cuh"
+#include "attend_common.cuh"
 
 namespace speca {
 
-using namespace tc;
+using namespace attend;
 
 namespace {
 
-constexpr int kMaxCtas = 160;            // pieces of the list at most (148 SMs)
-constexpr int kRecords = 4;              // ring of segment records
 constexpr float kSlack = 8.f;            // binary digits a maximum may grow by before O is scaled
-constexpr int kFlagRing = 8;
 
 // D <= 128: two softmax groups of 128 rows, each with an O and a buffer for S of its own.  A unit of at most 128 rows has its
 // even key tiles in one and the odd ones in the other, joined at the end; a larger one has a row tile in each, over the same
 // keys.  D = 256: O alone takes half of TMEM, and there is one group, over tiles of half as many keys in three buffers.
 // P takes the first half of the columns of its S.  One warp asks for scores, another for the products with V, so that neither's waits
 // hold the other up (a loop over one item takes 1200 cycles beside its 12 products where one warp does both).
-template <int D> struct Cfg {
+template <int DH> struct Cfg {
+    static constexpr int D = DH;
     static constexpr int N = D == 256 ? 64 : 128;
     static constexpr int LANES = D == 256 ? 1 : 2;
     static constexpr int BUFS = LANES == 2 ? 2 : 3;
     static constexpr int MT = 128 * LANES;
-    static constexpr int SOFT = 4 * LANES;                   // softmax warps; then TMA, scores, products with V, mending of V, schedule
-    static constexpr int THREADS = (SOFT + 5) * 32;
+    static constexpr int kEnds = D == 256 ? 5 : 3;           // a unit's beginning and end in tiles: 8000 to 17000 cycles, a tile 2500 to 3500
+    static constexpr bool kMend = true;
+    static constexpr int SOFT = 4 * LANES;                   // softmax warps; then keys, scores, products with V, mending of V, schedule, values
+    static constexpr int THREADS = (SOFT + 6) * 32;
     static constexpr int Q_BYTES = 128 * D * 2;
     static constexpr int TILE = N * D * 2;                   // keys or values of a tile
     static constexpr int KS = D == 64 ? 5 : 2, VS = D == 64 ? 5 : 3;       // tiles of keys and of values in flight or in use
@@ -54,36 +53,6 @@ template <int D> struct Cfg {
 static_assert(Cfg<128>::Bytes <= 232448 && Cfg<256>::Bytes <= 232448 && Cfg<64>::Bytes <= 232448, "shared memory of a CTA");
 
 constexpr int kTmemCols = 512, kOCol = 256;                  // S (P) buffers from 0, N columns each, O from column 256
-
-// A piece of one unit: key tiles t0 .. t1-1, of which the first `ct` of the unit are the cache's.
-struct Rec {
-    int l, b, hk, base;
-    int n, len, row0, rows;
-    int t0, t1, ct, nodes;                                   // nodes: draft nodes the unit's rows can see (0 .. nodes-1)
-    int slot, index, pad0, pad1;                             // slot: -1 the whole unit, 0 / 1 where its sums go
-};
-static_assert(sizeof(Rec) == 64, "record");
-
-// Joining: what a CTA's unit that goes on in the next CTAs needs.
-struct Join {
-    int parts, l, hk, base;
-    int row0, rows, pad0, pad1;
-};
-
-struct Plan {
-    int rows_cap;                                            // rows of a slot
-    size_t slot_bytes;
-    Join *join;
-    char *slots;
-};
-
-__host__ __device__ inline size_t slot_bytes(int rows, int d) { return align256(size_t(rows) * d * 4 + size_t(rows) * 8 + 16); }
-inline int slot_rows(int max_nodes, int group, int mt) { return int(1LL * max_nodes * group < mt ? 1LL * max_nodes * group : mt); }
-
-__device__ __forceinline__ float *slot_sums(const Plan &pl, int cta, int slot)
-{
-    return reinterpret_cast<float *>(pl.slots + (size_t(cta) * 2 + slot) * pl.slot_bytes);
-}
 
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float *r)
 {
@@ -141,13 +110,6 @@ __device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, ui
         ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(lead)
         : "memory");
 }
-// A tile of keys or values in shared memory: groups of eight rows, in a group one 64-wide block of columns behind the other,
-// in a block eight rows of 128 bytes with the 128-byte swizzle.  So one copy brings a page whatever its width (with the blocks
-// outermost it takes one a block, and 32 copies a tile of 16-row pages and 128 columns took longer than the tile's bytes).
-template <int D> __device__ __forceinline__ uint32_t tile_offset(int row, int chunk)       // of 16 bytes
-{
-    return uint32_t((row >> 3) * (D / 64) + (chunk >> 3)) * 1024u + (row & 7) * 128 + (((chunk & 7) ^ (row & 7)) << 4);
-}
 // operand whose rows are M or N (keys of S = Q K^T), `group` bytes between groups of eight rows
 __device__ __forceinline__ uint64_t make_desc_k(uint32_t smem_addr, uint32_t group)
 {
@@ -158,37 +120,6 @@ __device__ __forceinline__ uint64_t make_desc_k(uint32_t smem_addr, uint32_t gro
 __device__ __forceinline__ uint64_t make_desc_mn(uint32_t smem_addr, uint32_t group)
 {
     return (make_desc_k(smem_addr, group) & ~(uint64_t(0x3fff) << 16)) | uint64_t(1024 >> 4) << 16;
-}
-// as tma_load_3d, by the lane that has `lead` set
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int w, uint32_t bar, uint32_t lead)
-{
-    asm volatile(
-        "{\n\t.reg .pred q;\n\t"
-        "setp.ne.b32 q, %7, 0;\n\t"
-        "@q cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}"
-        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar), "r"(lead)
-        : "memory");
-}
-__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int w, int v, uint32_t bar, uint32_t lead)
-{
-    asm volatile(
-        "{\n\t.reg .pred q;\n\t"
-        "setp.ne.b32 q, %8, 0;\n\t"
-        "@q cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];\n\t}"
-        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(v), "r"(bar), "r"(lead)
-        : "memory");
-}
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
-{
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-__device__ __forceinline__ float exp2_approx(float x)
-{
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
 }
 __device__ __forceinline__ float max3(float a, float b, float c)
 {
@@ -216,177 +147,41 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
-// 16 bytes from global to shared memory, none of a thread's copies waits for another
-__device__ __forceinline__ void copy16(uint32_t dst, const void *src)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void copy16_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-__device__ __forceinline__ bool not_finite(uint32_t pair)
-{
-    return (pair & 0x7f80u) == 0x7f80u || (pair & 0x7f800000u) == 0x7f800000u;
-}
-
-// ---------------------------------------------------------------------------------------------------------------
-// The list of tiles
-// ---------------------------------------------------------------------------------------------------------------
-struct Seq {
-    int base, n, len, ct, fault;
-};
-
-template <int N> __device__ __forceinline__ Seq sequence(const AttnParams &p, int b)
-{
-    Seq s;
-    s.fault = sequence_nodes(p, b, s.base, s.n);
-    s.len = p.kv_len[b];
-    if (s.len < 0 || (s.len >> p.page_shift) > p.max_pages || s.len > p.max_pages << p.page_shift) s.fault |= SPECA_STATUS_BAD_PAGE;
-    if (s.fault) s.n = 0;
-    s.ct = s.fault ? 0 : (s.len + N - 1) / N;
-    return s;
-}
-// draft nodes that the rows of row tile m can see
-template <int MT> __device__ __forceinline__ int nodes_seen(int n, int group, int m)
-{
-    return min(n, ((m + 1) * MT - 1) / group + 1);
-}
-template <int D> __device__ __forceinline__ long unit_tiles(const Seq &s, int group, int m)
-{
-    return s.ct + (nodes_seen<Cfg<D>::MT>(s.n, group, m) + Cfg<D>::N - 1) / Cfg<D>::N;
-}
-// Cost of a unit, in tiles of 128 rows: its own (twice as many where two row tiles share the keys) and what begins and ends it,
-// queries in, sums out, the pipeline filled and drained (8000 to 17000 cycles, a tile 2500 to 3500).  Pieces are equal in this
-// measure: with tiles alone counted, CTAs that got many short sequences took up to twice as long as the others.
-template <int D> struct Cost {
-    static constexpr int kEnds = D == 256 ? 5 : 3;
-};
-template <int D> __device__ __forceinline__ int tile_cost(const Seq &s, int group, int m)
-{
-    return Cfg<D>::LANES == 2 && s.n * group - m * Cfg<D>::MT > 128 ? 2 : 1;
-}
-template <int D> __device__ __forceinline__ long unit_cost(const Seq &s, int group, int m)
-{
-    return unit_tiles<D>(s, group, m) * tile_cost<D>(s, group, m) + Cost<D>::kEnds;
-}
-template <int D> __device__ __forceinline__ int row_tiles(const Seq &s, int group)
-{
-    return (s.n * group + Cfg<D>::MT - 1) / Cfg<D>::MT;     // (at most 8192 nodes and 65536 heads)
-}
-// cost of one layer and key head
-template <int D> __device__ __forceinline__ long head_cost(const Seq &s, int group)
-{
-    long sum = 0;
-    for (int m = 0; m < row_tiles<D>(s, group); ++m) sum += unit_cost<D>(s, group, m);
-    return sum;
-}
-
 template <int D>
 __global__ void __launch_bounds__(Cfg<D>::THREADS, 1)
-attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
-              const __grid_constant__ CUtensorMap kd_map, const __grid_constant__ CUtensorMap vd_map, AttnParams p, Plan plan,
-              int32_t box_rows)
+attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_t box_rows)
 {
     after_previous_kernel();
     using C = Cfg<D>;
     constexpr int N = C::N, LANES = C::LANES, BUFS = C::BUFS, SOFT = C::SOFT, KS = C::KS, VS = C::VS;
     extern __shared__ __align__(1024) uint8_t smem[];
-    const uint32_t sbase = smem_u32(smem);
+    Cta<C> x(p, plan, smem);
+    const uint32_t sbase = x.sbase;
     if (sbase & 1023u) {                                     // never expected; refuse to run rather than corrupt
         if (threadIdx.x == 0) atomicOr(p.status, SPECA_STATUS_TIMEOUT);
         return;
     }
-    auto bar = [&](int i) { return sbase + C::OffBars + 8u * uint32_t(i); };
-    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + C::OffMisc);
+    auto bar = [&](int i) { return x.bar(i); };
+    volatile int *const abort_flag = x.abort_flag, *const topo_bad = x.topo_bad;
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + C::OffMisc + 4);
-    volatile int *topo_bad = reinterpret_cast<volatile int *>(smem + C::OffMisc + 8);      // [2]
-    volatile int *start = reinterpret_cast<volatile int *>(smem + C::OffMisc + 16);        // sequence, then tiles into it (64 bits)
-    volatile int *page_bad = reinterpret_cast<volatile int *>(smem + C::OffFlags);         // [kFlagRing] 1 + segment number
-    volatile int *value_bad = page_bad + kFlagRing;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int group = p.H / p.HK;
-    const int grid = gridDim.x, cta = blockIdx.x;
+    const int warp = x.warp, lane = x.lane, group = x.group, cta = blockIdx.x;
 
     if (threadIdx.x == 0) {
-        *abort_flag = 0;
-        topo_bad[0] = topo_bad[1] = 0;
-        for (int i = 0; i < 2 * kFlagRing; ++i) page_bad[i] = 0;
-        for (int i = 0; i < KS; ++i) { mbar_init(bar(C::kKFull + i), 1); mbar_init(bar(C::kKEmpty + i), 1); }
-        for (int i = 0; i < VS; ++i) { mbar_init(bar(C::kVFull + i), 1); mbar_init(bar(C::kVEmpty + i), 1); mbar_init(bar(C::kVRaw + i), 1); }
+        x.init(SOFT + 5, 1);
+        for (int i = 0; i < VS; ++i) mbar_init(bar(C::kVRaw + i), 1);
         for (int i = 0; i < BUFS; ++i) { mbar_init(bar(C::kSFull + i), 1); mbar_init(bar(C::kPReady + i), 4); mbar_init(bar(C::kODone + i), 1); }
         mbar_init(bar(C::kQFull), SOFT);
         mbar_init(bar(C::kSync), SOFT);
-        for (int i = 0; i < kRecords; ++i) { mbar_init(bar(C::kRecFull + i), 1); mbar_init(bar(C::kRecEmpty + i), SOFT + 4); }
         mbar_init(bar(C::kDrain), 2);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == SOFT + 1) tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_slot)), kTmemCols);
 
-    // ---- cost of the whole list, and where this CTA's piece begins: every thread has some consecutive sequences
-    long mine = 0, before = 0, total = 0;
-    const int per_thread = (p.B + C::THREADS - 1) / C::THREADS;
-    const int b_lo = min(p.B, int(threadIdx.x) * per_thread), b_hi = min(p.B, b_lo + per_thread);
-    const long heads = long(p.L) * p.HK;
-    for (int b = b_lo; b < b_hi; ++b) {
-        const Seq s = sequence<N>(p, b);
-        if (s.fault && cta == 0) atomicOr(p.status, s.fault);
-        mine += heads * head_cost<D>(s, group);
-    }
-    long incl = mine;
-#pragma unroll
-    for (int i = 1; i < 32; i *= 2) {
-        const long x = __shfl_up_sync(0xffffffffu, incl, i);
-        if (lane >= i) incl += x;
-    }
-    volatile long *sums = reinterpret_cast<volatile long *>(smem + C::OffPar);
-    if (lane == 31) sums[warp] = incl;
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    for (int w = 0; w < C::THREADS / 32; ++w) {
-        if (w < warp) before += sums[w];
-        total += sums[w];
-    }
-    before += incl - mine;
-    // (a piece is at least one tile long, so that every CTA between a unit's first and last has some of it)
-    const int pieces = int(min(long(grid), max(1L, total / (plan.rows_cap > 128 ? 2 : 1))));
-    const long per = total / pieces, extra = total % pieces;
-    const long begin = cta * per + min(long(cta), extra), count = cta < pieces ? per + (cta < extra ? 1 : 0) : 0;
-    if (count > 0 && begin >= before && begin < before + mine) {
-        long rem = begin - before;
-        int b = b_lo;
-        for (;; ++b) {
-            const long t = heads * head_cost<D>(sequence<N>(p, b), group);
-            if (rem < t) break;
-            rem -= t;
-        }
-        start[0] = b;
-        start[2] = int(rem & 0xffffffffL);
-        start[3] = int(rem >> 32);
-    }
-    __syncthreads();
-    const uint32_t tmem = *tmem_slot;
-    const uint32_t lead = elect_one();
-    bool ok = true;
-
-    // record of segment `s`; false: the list has ended, or (ok == false) the CTA is aborting
-    auto record = [&](uint32_t s, Rec &r) -> bool {
-        if (!(ok = wait_fast(bar(C::kRecFull + (s % kRecords)), (s / kRecords) & 1, abort_flag))) return false;
-        const int4 *src = reinterpret_cast<const int4 *>(smem + C::OffRec) + 4 * (s % kRecords);
-        const int4 a = src[0], b = src[1], c = src[2], d = src[3];
-        r = Rec{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w, c.x, c.y, c.z, c.w, d.x, d.y, 0, 0};
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(C::kRecEmpty + (s % kRecords)));
-        return r.rows > 0;
-    };
-    // rows of tile t that hold keys
-    auto valid_of = [&](const Rec &r, int t) {
-        const int left = t < r.ct ? r.len - t * N : r.nodes - (t - r.ct) * N;
-        return left < N ? left : N;
-    };
-    // (A barrier has two parities: whoever waits on one waits for all its phases in turn.  So keys and values have rings of
-    // their own, and values that are looked over before they are used land on a barrier of their own.)
-    // (a chain's draft keys below the first of the unit's nodes: every row attends them all)
-    auto all_seen = [&](const Rec &r, int t) { return t < r.ct || (p.parent == nullptr && (t - r.ct + 1) * N <= r.row0 / group + 1); };
-    auto to_mend = [&](const Rec &r, int t) { return (valid_of(r, t) & 15) != 0 || !all_seen(r, t); };
+    x.find_piece();
+    const uint32_t tmem = *tmem_slot, lead = x.lead;
+    bool &ok = x.ok;
+    auto record = [&](uint32_t s, Rec &r) { return x.record(s, r); };
+    auto valid_of = [&](const Rec &r, int t) { return x.valid_of(r, t); };
     // Buffer of item i of a segment.  Every use of a buffer is one phase of its three barriers (scores there, weights there,
     // weights used); a role keeps the parity of the next one, a bit a buffer.
     auto buffer = [](int i) { return LANES == 2 ? i & 1 : i % 3; };
@@ -394,64 +189,7 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
 
     if (warp == SOFT) {
         // ------------------------------------------------------------------------------- keys and values, by TMA
-        uint32_t nk = 0, nv = 0;
-        for (uint32_t seg = 0; ok && record(seg, r); ++seg) {
-            const int32_t *table = p.page_table + size_t(r.b) * p.max_pages;
-            const int pages = (r.len + (1 << p.page_shift) - 1) >> p.page_shift;
-            int window = (r.t0 * N) >> p.page_shift;         // 32 entries of the table, one a lane, and the 32 behind them
-            auto entries = [&](int first) { return r.t0 < r.ct && first + lane < pages ? table[first + lane] : 0; };
-            int ids = entries(window), next = entries(window + 32);
-            const int tiles = r.t1 - r.t0;
-            int mine = 0, last = 0;                          // this lane's page of the tile, and of the tile before it
-#pragma unroll 1
-            for (int i = 0; i <= tiles && ok; ++i) {
-                const int t = r.t0 + i;
-                last = mine;
-                if (i < tiles && t < r.ct) {
-                    const int page = (t * N + lane * box_rows) >> p.page_shift, first = (t * N) >> p.page_shift;
-                    if (first >= window + 32) {
-                        window = first;
-                        ids = next;
-                        next = entries(window + 32);
-                    }
-                    mine = __shfl_sync(0xffffffffu, ids, (page - window) & 31);
-                    if (lane * box_rows < valid_of(r, t) && (mine < 0 || mine >= p.n_pages)) {
-                        mine = 0;                            // read what is there, and leave the unit's outputs alone
-                        page_bad[seg % kFlagRing] = int(seg) + 1;
-                        atomicOr(p.status, SPECA_STATUS_BAD_PAGE);
-                    }
-                }
-                // keys of this tile, then values of the one before
-#pragma unroll
-                for (int kv = 0; kv < 2; ++kv) {
-                    const int tt = t - kv;
-                    if (kv ? i == 0 : i == tiles) continue;
-                    const int n = kv ? nv : nk, s = kv ? n % VS : n % KS, round = kv ? n / VS : n / KS;
-                    if (!(ok = wait_fast(bar((kv ? C::kVEmpty : C::kKEmpty) + s), (round & 1) ^ 1, abort_flag))) break;
-                    (kv ? nv : nk) = n + 1;
-                    const int valid = valid_of(r, tt);
-                    const uint32_t full = bar((kv == 0 ? C::kKFull : to_mend(r, tt) ? C::kVRaw : C::kVFull) + s);
-                    const uint32_t dst = sbase + C::OffRing + (kv ? KS + s : s) * C::TILE;
-                    if (tt >= r.ct) {
-                        const int boxes = (valid + 7) / 8, row = r.l * p.T + r.base + (tt - r.ct) * N;
-                        if (lead) mbar_arrive_expect_tx(full, uint32_t(boxes) * (8 * D * 2));
-                        __syncwarp();
-#pragma unroll 1
-                        for (int j = 0; j < boxes; ++j)
-                            tma_load_4d(dst + j * (8 * D * 2), kv ? &vd_map : &kd_map, 0, row + 8 * j, 0, r.hk, full, lead);
-                    } else {
-                        const int boxes = (valid + box_rows - 1) / box_rows, group = ((tt * N) & ((1 << p.page_shift) - 1)) >> 3;
-                        if (lead) mbar_arrive_expect_tx(full, uint32_t(boxes) * box_rows * (D * 2));
-                        __syncwarp();
-#pragma unroll 1
-                        for (int j = 0; j < boxes; ++j) {
-                            const int id = __shfl_sync(0xffffffffu, kv ? last : mine, j);
-                            tma_load_5d(dst + j * box_rows * (D * 2), kv ? &v_map : &k_map, 0, 0, 0, group, (r.l * p.n_pages + id) * p.HK + r.hk, full, lead);
-                        }
-                    }
-                }
-            }
-        }
+        x.load<0>(maps, box_rows);
     } else if (warp == SOFT + 1) {
         // ------------------------------------------------------------------------------- scores
         const uint32_t id_s = make_idesc_bf16(N);
@@ -515,9 +253,9 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
         for (uint32_t seg = 0; ok && record(seg, r); loads += r.t1 - r.t0, ++seg) {
 #pragma unroll 1
             for (int t = r.t0; t < r.t1; ++t) {
-                if (!to_mend(r, t)) continue;
+                if (!x.to_mend(r, t)) continue;
                 const int valid = valid_of(r, t);
-                const bool draft = !all_seen(r, t);
+                const bool draft = !x.all_seen(r, t);
                 const uint32_t s = (loads + (t - r.t0)) % VS;
                 if (!(ok = wait_fast(bar(C::kVRaw + s), (phase >> s) & 1, abort_flag))) break;
                 phase ^= 1u << s;
@@ -545,7 +283,7 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
                             bad = true;
                         }
                     }
-                    if (bad) value_bad[seg % kFlagRing] = int(seg) + 1;
+                    if (bad) x.value_bad[seg % kFlagRing] = int(seg) + 1;
                 }
                 fence_proxy_async();
                 __syncwarp();
@@ -554,66 +292,9 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
         }
     } else if (warp == SOFT + 4) {
         // ------------------------------------------------------------------------------- schedule
-        Join join{0, 0, 0, 0, 0, 0, 0, 0};
-        uint32_t seg = 0;
-        auto put = [&](const Rec &x) {
-            ok = seg < kRecords || wait_fast(bar(C::kRecEmpty + (seg % kRecords)), ((seg / kRecords) & 1) ^ 1, abort_flag);
-            if (!ok) return;
-            if (lane == 0) {
-                *reinterpret_cast<Rec *>(smem + C::OffRec + 64 * (seg % kRecords)) = x;
-                mbar_arrive(bar(C::kRecFull + (seg % kRecords)));
-            }
-            __syncwarp();
-            ++seg;
-        };
-        long left = count;
-        if (left > 0) {
-            int b = start[0];
-            long in = (long(start[3]) << 32) | uint32_t(start[2]);       // place in the sequence where the piece begins
-            for (; left > 0 && ok; ++b, in = 0) {
-                const Seq s = sequence<N>(p, b);
-                const long hc = head_cost<D>(s, group);
-                if (hc == 0) continue;
-                const int mts = row_tiles<D>(s, group);
-                long hd = in / hc;
-                in -= hd * hc;
-                for (; hd < heads && left > 0 && ok; ++hd) {
-                    for (int m = 0; m < mts && left > 0 && ok; ++m) {
-                        const long uc = unit_cost<D>(s, group, m);
-                        if (in >= uc) { in -= uc; continue; }
-                        // the unit's ends stand before its tiles; a tile is whose piece its beginning is in
-                        const int ut = int(unit_tiles<D>(s, group, m)), w = tile_cost<D>(s, group, m);
-                        auto tile_at = [&](long x) { return int(min(long(ut), max(0L, (x - Cost<D>::kEnds + w - 1) / w))); };
-                        const long take = min(left, uc - in);
-                        Rec x{};
-                        x.t0 = tile_at(in);
-                        x.t1 = tile_at(in + take);
-                        if (x.t1 > x.t0) {
-                            x.l = int(hd / p.HK); x.b = b; x.hk = int(hd % p.HK); x.base = s.base; x.n = s.n; x.len = s.len;
-                            x.row0 = m * C::MT;
-                            x.rows = min(C::MT, s.n * group - x.row0);
-                            x.ct = s.ct;
-                            x.nodes = nodes_seen<C::MT>(s.n, group, m);
-                            x.slot = x.t0 == 0 && x.t1 == ut ? -1 : x.t0 == 0 ? 1 : 0;
-                            if (x.slot == 1) {
-                                // the unit ends in a later CTA's piece: where its last tile begins
-                                const long last = begin + (count - left) - in + Cost<D>::kEnds + long(ut - 1) * w, wide = extra * (per + 1);
-                                const int owner = int(last < wide ? last / (per + 1) : extra + (last - wide) / per);
-                                join = Join{owner - cta + 1, x.l, x.hk, x.base, x.row0, x.rows, 0, 0};
-                            }
-                            put(x);
-                        }
-                        left -= take;
-                        in = 0;
-                    }
-                }
-            }
-        }
-        if (ok) put(Rec{});
-        if (lane == 0) {
-            if (!ok) join.parts = 0;
-            plan.join[cta] = join;
-        }
+        x.schedule();
+    } else if (warp == SOFT + 5) {
+        x.load<1>(maps, box_rows);
     } else {
         // ------------------------------------------------------------------------------- softmax, and what is written
         const int wg = warp >> 2, quad = warp & 3, trow = quad * 32 + lane;      // lane of TMEM: row of this group's tile
@@ -674,7 +355,7 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
                 if (live) {
                     const uint32_t ta = tq + buf * N;
                     const int valid = valid_of(r, t);
-                    const bool masked = valid < N || !all_seen(r, t);
+                    const bool masked = valid < N || !x.all_seen(r, t);
                     uint32_t mask[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
                     if (masked) {
                         const int first = (t - r.ct) * N;    // first node of a draft tile
@@ -806,8 +487,8 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
                 ll = a.y * f0 + (all > 1 ? b.y * f1 : 0.f);
             }
             const bool bad = topo_bad[seg & 1] != 0 && p.parent != nullptr && r.t1 > r.ct;
-            const bool skip = bad || page_bad[seg % kFlagRing] == int(seg) + 1;
-            const bool mend = value_bad[seg % kFlagRing] == int(seg) + 1;
+            const bool skip = bad || x.page_bad[seg % kFlagRing] == int(seg) + 1;
+            const bool mend = x.value_bad[seg % kFlagRing] == int(seg) + 1;
             if (live) {
                 const uint32_t o0 = tq + kOCol + (LANES == 2 && two ? wg * D : 0), o1 = tq + kOCol + D;
                 const bool both = merge && all > 1;
@@ -894,7 +575,7 @@ attend_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
         mma_commit(bar(C::kDrain), lead);
         mbar_wait(bar(C::kDrain), 0, abort_flag);
     }
-    if (warp == SOFT && *abort_flag) {
+    if ((warp == SOFT || warp == SOFT + 5) && *abort_flag) {
         // let copies still in flight land before the CTA's shared memory goes away
         const uint64_t t0 = global_timer_ns();
         while (global_timer_ns() - t0 < 200000ull) __nanosleep(1000);
@@ -957,13 +638,19 @@ join_kernel(AttnParams p, Plan plan, int32_t blocks)
     for (int e = 0; e < E; e += 2) *reinterpret_cast<uint32_t *>(to + e) = pack_bf16(o[e] * inv, o[e + 1] * inv);
 }
 
+// rows of a unit at most
+inline int unit_rows(int max_nodes, int group, int d)
+{
+    const long rows = long(max_nodes) * group;
+    const int few = attend_few_rows(d, rows), mt = few > 0 ? few : d == 256 ? Cfg<256>::MT : Cfg<128>::MT;
+    return rows < mt ? int(rows) : mt;
+}
+
 std::atomic<bool> g_opted_in[64];                            // per device: shared memory of every instantiation
 
 template <int D> int launch_width(const AttnParams &p, cudaStream_t st)
 {
     using C = Cfg<D>;
-    EncodeTiledFn encode = encode_tiled_fn();
-    if (encode == nullptr) return int(cudaErrorNotSupported);
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return int(cudaErrorInvalidDevice);
     const int sms = sm_count_of_current_device();
@@ -977,30 +664,16 @@ template <int D> int launch_width(const AttnParams &p, cudaStream_t st)
         if (e != cudaSuccess) return int(e);
         g_opted_in[dev].store(true, std::memory_order_release);
     }
-    const int page = 1 << p.page_shift, box_rows = page < C::N ? page : C::N;
-    CUtensorMap maps[4];
-    const cuuint32_t es[5] = {1, 1, 1, 1, 1};
-    for (int i = 0; i < 4; ++i) {
-        const bool cache = i < 2;
-        const void *base = i == 0 ? p.k_cache : i == 1 ? p.v_cache : i == 2 ? p.k : p.v;
-        // 64 columns, eight rows, blocks of columns; of the cache groups of eight rows and (layer, page, head) besides, of the
-        // draft rows of all layers in place of the eight, and the head
-        const cuuint64_t row = cuuint64_t(D) * 2 * (cache ? 1 : p.HK);
-        const cuuint64_t dim[5] = {64, cache ? 8u : cuuint64_t(p.L) * p.T, D / 64, cuuint64_t(cache ? page / 8 : p.HK), cuuint64_t(p.L) * p.n_pages * p.HK};
-        const cuuint64_t stride[4] = {row, 128, cache ? 8 * row : cuuint64_t(D) * 2, cuuint64_t(page) * D * 2};
-        const cuuint32_t box[5] = {64, 8, D / 64, cuuint32_t(cache ? box_rows / 8 : 1), 1};
-        if (encode(&maps[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, cache ? 5 : 4, const_cast<void *>(base), dim, stride, box, es,
-                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-            return int(cudaErrorInvalidValue);
-    }
-    Plan plan;
-    plan.rows_cap = slot_rows(p.max_nodes, p.H / p.HK, C::MT);
-    plan.slot_bytes = slot_bytes(plan.rows_cap, D);
-    plan.join = static_cast<Join *>(p.workspace);
-    plan.slots = static_cast<char *>(p.workspace) + align256(sizeof(Join) * kMaxCtas);
-    const int grid = sms < kMaxCtas ? sms : kMaxCtas;
-    launch(attend_kernel<D>, grid, C::THREADS, C::Bytes, st, maps[0], maps[1], maps[2], maps[3], p, plan, int32_t(box_rows));
+    const int page = 1 << p.page_shift, box_rows = page < C::N ? page : C::N, grid = sms < kMaxCtas ? sms : kMaxCtas;
+    Maps maps;
+    const int rc = encode_maps<D>(p, box_rows, maps);
+    if (rc != 0) return rc;
+    const Plan plan = make_plan(p, unit_rows(p.max_nodes, p.H / p.HK, D), D);
+    const int few = attend_few_rows(D, long(p.max_nodes) * (p.H / p.HK));
+    if (few > 0) {
+        const int r = launch_attend_few(p, D, few, maps, plan, box_rows, grid, st);
+        if (r != 0) return r;
+    } else launch(attend_kernel<D>, grid, C::THREADS, C::Bytes, st, maps, p, plan, int32_t(box_rows));
     const int e = int(cudaGetLastError());
     if (e != 0) return e;
     const int blocks = (plan.rows_cap + kJoinWarps - 1) / kJoinWarps;
@@ -1012,8 +685,7 @@ template <int D> int launch_width(const AttnParams &p, cudaStream_t st)
 
 size_t attend_workspace_bytes(const speca_attn_dims *d)
 {
-    const int mt = d->d_head == 256 ? Cfg<256>::MT : Cfg<128>::MT;
-    return align256(sizeof(Join) * kMaxCtas) + 2 * kMaxCtas * slot_bytes(slot_rows(d->max_nodes, d->heads / d->kv_heads, mt), d->d_head);
+    return align256(sizeof(Join) * kMaxCtas) + 2 * kMaxCtas * slot_bytes(unit_rows(d->max_nodes, d->heads / d->kv_heads, d->d_head), d->d_head);
 }
 
 int launch_attend(const AttnParams &p, int d_head, cudaStream_t st)

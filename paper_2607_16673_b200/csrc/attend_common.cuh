@@ -1,0 +1,429 @@
+// What the attention kernels share: the list of work and its equal pieces, the warp that schedules a CTA's piece, the warp that
+// brings keys and values in.
+#pragma once
+
+#include "attn.cuh"
+#include "tc_ptx.cuh"
+
+namespace speca {
+namespace attend {
+
+using namespace tc;
+
+constexpr int kMaxCtas = 160;            // pieces of the list at most (148 SMs)
+constexpr int kRecords = 4;              // ring of segment records
+constexpr int kFlagRing = 8;
+
+// A piece of one unit: key tiles t0 .. t1-1, of which the first `ct` of the unit are the cache's.
+struct Rec {
+    int l, b, hk, base;
+    int n, len, row0, rows;
+    int t0, t1, ct, nodes;                                   // nodes: draft nodes the unit's rows can see (0 .. nodes-1)
+    int slot, index, pad0, pad1;                             // slot: -1 the whole unit, 0 / 1 where its sums go
+};
+static_assert(sizeof(Rec) == 64, "record");
+
+// Joining: what a CTA's unit that goes on in the next CTAs needs.
+struct Join {
+    int parts, l, hk, base;
+    int row0, rows, pad0, pad1;
+};
+
+struct Plan {
+    int rows_cap;                                            // rows of a slot
+    size_t slot_bytes;
+    Join *join;
+    char *slots;
+};
+
+__host__ __device__ inline size_t slot_bytes(int rows, int d) { return align256(size_t(rows) * d * 4 + size_t(rows) * 8 + 16); }
+
+__device__ __forceinline__ float *slot_sums(const Plan &pl, int cta, int slot)
+{
+    return reinterpret_cast<float *>(pl.slots + (size_t(cta) * 2 + slot) * pl.slot_bytes);
+}
+
+// A tile of keys or values in shared memory: groups of eight rows, in a group one 64-wide block of columns behind the other,
+// in a block eight rows of 128 bytes with the 128-byte swizzle.  So one copy brings a page whatever its width (with the blocks
+// outermost it takes one a block, and 32 copies a tile of 16-row pages and 128 columns took longer than the tile's bytes).
+template <int D> __device__ __forceinline__ uint32_t tile_offset(int row, int chunk)       // of 16 bytes
+{
+    return uint32_t((row >> 3) * (D / 64) + (chunk >> 3)) * 1024u + (row & 7) * 128 + (((chunk & 7) ^ (row & 7)) << 4);
+}
+// as tma_load_3d, by the lane that has `lead` set
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int w, uint32_t bar, uint32_t lead)
+{
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "setp.ne.b32 q, %7, 0;\n\t"
+        "@q cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}"
+        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar), "r"(lead)
+        : "memory");
+}
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int w, int v, uint32_t bar, uint32_t lead)
+{
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "setp.ne.b32 q, %8, 0;\n\t"
+        "@q cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];\n\t}"
+        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(v), "r"(bar), "r"(lead)
+        : "memory");
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ float exp2_approx(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// 16 bytes from global to shared memory, none of a thread's copies waits for another
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy16_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ bool not_finite(uint32_t pair)
+{
+    return (pair & 0x7f80u) == 0x7f80u || (pair & 0x7f800000u) == 0x7f800000u;
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// The list of tiles
+// ---------------------------------------------------------------------------------------------------------------
+struct Seq {
+    int base, n, len, ct, fault;
+};
+
+template <class C> __device__ __forceinline__ Seq sequence(const AttnParams &p, int b)
+{
+    Seq s;
+    s.fault = sequence_nodes(p, b, s.base, s.n);
+    s.len = p.kv_len[b];
+    if (s.len < 0 || (s.len >> p.page_shift) > p.max_pages || s.len > p.max_pages << p.page_shift) s.fault |= SPECA_STATUS_BAD_PAGE;
+    if (s.fault) s.n = 0;
+    s.ct = s.fault ? 0 : (s.len + C::N - 1) / C::N;
+    return s;
+}
+// draft nodes that the rows of row tile m can see
+template <int MT> __device__ __forceinline__ int nodes_seen(int n, int group, int m)
+{
+    return min(n, ((m + 1) * MT - 1) / group + 1);
+}
+template <class C> __device__ __forceinline__ long unit_tiles(const Seq &s, int group, int m)
+{
+    return s.ct + (nodes_seen<C::MT>(s.n, group, m) + C::N - 1) / C::N;
+}
+// Cost of a unit, in tiles: its own (twice as many where two row tiles share the keys) and what begins and ends it, queries in,
+// sums out, the pipeline filled and drained.  Pieces are equal in this measure: with tiles alone counted, CTAs that got many
+// short sequences took up to twice as long as the others.
+template <class C> __device__ __forceinline__ int tile_cost(const Seq &s, int group, int m)
+{
+    return C::LANES == 2 && s.n * group - m * C::MT > 128 ? 2 : 1;
+}
+template <class C> __device__ __forceinline__ long unit_cost(const Seq &s, int group, int m)
+{
+    return unit_tiles<C>(s, group, m) * tile_cost<C>(s, group, m) + C::kEnds;
+}
+template <class C> __device__ __forceinline__ int row_tiles(const Seq &s, int group)
+{
+    return (s.n * group + C::MT - 1) / C::MT;     // (at most 8192 nodes and 65536 heads)
+}
+// cost of one layer and key head
+template <class C> __device__ __forceinline__ long head_cost(const Seq &s, int group)
+{
+    long sum = 0;
+    for (int m = 0; m < row_tiles<C>(s, group); ++m) sum += unit_cost<C>(s, group, m);
+    return sum;
+}
+
+
+struct Maps {
+    CUtensorMap k, v, k_draft, v_draft;
+};
+
+// A CTA's view of the work.  C: N keys a tile, D columns, MT rows of a unit, THREADS, kEnds, LANES, KS and VS slots of TILE bytes
+// at OffRing (keys, then values), barriers from OffBars, scratch of 8 * THREADS / 32 bytes at OffPar.
+// (A barrier has two parities: whoever waits on one waits for all its phases in turn.  So keys and values have rings of their
+// own, and where C::kMend, values that are looked over before they are used land on barriers of their own.)
+template <class C> struct Cta {
+    static constexpr int N = C::N, D = C::D, KS = C::KS, VS = C::VS;
+    const AttnParams &p;
+    const Plan &plan;
+    uint8_t *smem;
+    uint32_t sbase;
+    int warp, lane, group;
+    volatile int *abort_flag, *topo_bad, *page_bad, *value_bad;      // topo_bad [2], the others [kFlagRing]: 1 + segment number
+    long begin, count, per, extra;                           // this CTA's piece of the list
+    uint32_t lead;
+    bool ok;
+
+    __device__ __forceinline__ Cta(const AttnParams &p_, const Plan &plan_, uint8_t *smem_)
+        : p(p_), plan(plan_), smem(smem_), sbase(smem_u32(smem_)), warp(threadIdx.x >> 5), lane(threadIdx.x & 31), group(p_.H / p_.HK),
+          abort_flag(reinterpret_cast<volatile int *>(smem_ + C::OffMisc)), topo_bad(abort_flag + 2),
+          page_bad(reinterpret_cast<volatile int *>(smem_ + C::OffFlags)), value_bad(page_bad + kFlagRing), ok(true)
+    {
+    }
+    __device__ __forceinline__ uint32_t bar(int i) const { return sbase + C::OffBars + 8u * uint32_t(i); }
+    // by one thread, before the barriers' fence
+    __device__ __forceinline__ void init(int consumers, int empties)
+    {
+        *abort_flag = 0;
+        topo_bad[0] = topo_bad[1] = 0;
+        for (int i = 0; i < 2 * kFlagRing; ++i) page_bad[i] = 0;
+        for (int i = 0; i < KS; ++i) { mbar_init(bar(C::kKFull + i), 1); mbar_init(bar(C::kKEmpty + i), empties); }
+        for (int i = 0; i < VS; ++i) { mbar_init(bar(C::kVFull + i), 1); mbar_init(bar(C::kVEmpty + i), empties); }
+        for (int i = 0; i < kRecords; ++i) { mbar_init(bar(C::kRecFull + i), 1); mbar_init(bar(C::kRecEmpty + i), consumers); }
+    }
+
+    // record of segment `s`; false: the list has ended, or (ok == false) the CTA is aborting
+    __device__ __forceinline__ bool record(uint32_t s, Rec &r)
+    {
+        if (!(ok = wait_fast(bar(C::kRecFull + (s % kRecords)), (s / kRecords) & 1, abort_flag))) return false;
+        const int4 *src = reinterpret_cast<const int4 *>(smem + C::OffRec) + 4 * (s % kRecords);
+        const int4 a = src[0], b = src[1], c = src[2], d = src[3];
+        r = Rec{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w, c.x, c.y, c.z, c.w, d.x, d.y, 0, 0};
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::kRecEmpty + (s % kRecords)));
+        return r.rows > 0;
+    }
+    // rows of tile t that hold keys
+    __device__ __forceinline__ int valid_of(const Rec &r, int t) const
+    {
+        const int left = t < r.ct ? r.len - t * N : r.nodes - (t - r.ct) * N;
+        return left < N ? left : N;
+    }
+    // whether every row of the unit attends all keys of tile t (of a chain's draft those below its first node)
+    __device__ __forceinline__ bool all_seen(const Rec &r, int t) const
+    {
+        return t < r.ct || (p.parent == nullptr && (t - r.ct + 1) * N <= r.row0 / group + 1);
+    }
+    __device__ __forceinline__ bool to_mend(const Rec &r, int t) const
+    {
+        return C::kMend && ((valid_of(r, t) & 15) != 0 || !all_seen(r, t));
+    }
+
+    // Cost of the whole list, and this CTA's piece; whole CTA.
+    __device__ __forceinline__ void find_piece()
+    {
+        const int grid = gridDim.x, cta = blockIdx.x;
+        volatile int *start = abort_flag + 4;                // sequence, then place in it (64 bits)
+        // ---- cost of the whole list, and where this CTA's piece begins: every thread has some consecutive sequences
+        long mine = 0, before = 0, total = 0;
+        const int per_thread = (p.B + C::THREADS - 1) / C::THREADS;
+        const int b_lo = min(p.B, int(threadIdx.x) * per_thread), b_hi = min(p.B, b_lo + per_thread);
+        const long heads = long(p.L) * p.HK;
+        for (int b = b_lo; b < b_hi; ++b) {
+            const Seq s = sequence<C>(p, b);
+            if (s.fault && cta == 0) atomicOr(p.status, s.fault);
+            mine += heads * head_cost<C>(s, group);
+        }
+        long incl = mine;
+#pragma unroll
+        for (int i = 1; i < 32; i *= 2) {
+            const long x = __shfl_up_sync(0xffffffffu, incl, i);
+            if (lane >= i) incl += x;
+        }
+        volatile long *sums = reinterpret_cast<volatile long *>(smem + C::OffPar);
+        if (lane == 31) sums[warp] = incl;
+        tc_fence_before();
+        __syncthreads();
+        tc_fence_after();
+        for (int w = 0; w < C::THREADS / 32; ++w) {
+            if (w < warp) before += sums[w];
+            total += sums[w];
+        }
+        before += incl - mine;
+        // (a piece is at least one tile long, so that every CTA between a unit's first and last has some of it)
+        const int pieces = int(min(long(grid), max(1L, total / (plan.rows_cap > 128 ? 2 : 1))));
+        per = total / pieces;
+        extra = total % pieces;
+        begin = cta * per + min(long(cta), extra);
+        count = cta < pieces ? per + (cta < extra ? 1 : 0) : 0;
+        if (count > 0 && begin >= before && begin < before + mine) {
+            long rem = begin - before;
+            int b = b_lo;
+            for (;; ++b) {
+                const long t = heads * head_cost<C>(sequence<C>(p, b), group);
+                if (rem < t) break;
+                rem -= t;
+            }
+            start[0] = b;
+            start[2] = int(rem & 0xffffffffL);
+            start[3] = int(rem >> 32);
+        }
+        __syncthreads();
+        lead = elect_one();
+    }
+
+    // Keys (KV = 0) or values (KV = 1) into their ring, one warp each: a copy of a page of 16 rows is 220 cycles of its warp, so
+    // that one warp for both took longer over a tile of such pages than its bytes do.
+    template <int KV> __device__ __forceinline__ void load(const Maps &maps, int box_rows)
+    {
+        constexpr int SLOTS = KV ? VS : KS;
+        const CUtensorMap *const map = KV ? &maps.v : &maps.k, *const draft = KV ? &maps.v_draft : &maps.k_draft;
+        Rec r;
+        uint32_t n = 0;
+        for (uint32_t seg = 0; ok && record(seg, r); ++seg) {
+            const int32_t *table = p.page_table + size_t(r.b) * p.max_pages;
+            const int pages = (r.len + (1 << p.page_shift) - 1) >> p.page_shift;
+            int window = (r.t0 * N) >> p.page_shift;         // 32 entries of the table, one a lane, and the 32 behind them
+            auto entries = [&](int first) { return r.t0 < r.ct && first + lane < pages ? table[first + lane] : 0; };
+            int ids = entries(window), next = entries(window + 32);
+#pragma unroll 1
+            for (int t = r.t0; t < r.t1; ++t, ++n) {
+                int at = 0;                                  // this lane's page of the tile, as a row of the map
+                if (t < r.ct) {
+                    const int page = (t * N + lane * box_rows) >> p.page_shift, first = (t * N) >> p.page_shift;
+                    if (first >= window + 32) {
+                        window = first;
+                        ids = next;
+                        next = entries(window + 32);
+                    }
+                    int id = __shfl_sync(0xffffffffu, ids, (page - window) & 31);
+                    if (lane * box_rows < valid_of(r, t) && (id < 0 || id >= p.n_pages)) {
+                        id = 0;                              // read what is there, and leave the unit's outputs alone
+                        page_bad[seg % kFlagRing] = int(seg) + 1;
+                        atomicOr(p.status, SPECA_STATUS_BAD_PAGE);
+                    }
+                    at = (r.l * p.n_pages + id) * p.HK + r.hk;
+                }
+                const int s = n % SLOTS;
+                if (!(ok = wait_fast(bar((KV ? C::kVEmpty : C::kKEmpty) + s), ((n / SLOTS) & 1) ^ 1, abort_flag))) break;
+                const int valid = valid_of(r, t);
+                const uint32_t full = bar((KV == 0 ? C::kKFull : to_mend(r, t) ? C::kVRaw : C::kVFull) + s);
+                const uint32_t dst = sbase + C::OffRing + (KV ? KS + s : s) * C::TILE;
+                if (t >= r.ct) {
+                    const int boxes = (valid + 7) / 8, row = r.l * p.T + r.base + (t - r.ct) * N;
+                    if (lead) mbar_arrive_expect_tx(full, uint32_t(boxes) * (8 * D * 2));
+                    __syncwarp();
+#pragma unroll 1
+                    for (int j = 0; j < boxes; ++j) tma_load_4d(dst + j * (8 * D * 2), draft, 0, row + 8 * j, 0, r.hk, full, lead);
+                } else {
+                    const int boxes = (valid + box_rows - 1) / box_rows, rows = ((t * N) & ((1 << p.page_shift) - 1)) >> 3;
+                    if (lead) mbar_arrive_expect_tx(full, uint32_t(boxes) * box_rows * (D * 2));
+                    __syncwarp();
+#pragma unroll 1
+                    for (int j = 0; j < boxes; ++j)
+                        tma_load_5d(dst + j * box_rows * (D * 2), map, 0, 0, 0, rows, __shfl_sync(0xffffffffu, at, j), full, lead);
+                }
+            }
+        }
+    }
+
+    // Records of the piece, one warp, and what the join needs of it.
+    __device__ __forceinline__ void schedule()
+    {
+        const int cta = blockIdx.x;
+        const long heads = long(p.L) * p.HK;
+        volatile int *start = abort_flag + 4;
+        Join join{0, 0, 0, 0, 0, 0, 0, 0};
+        uint32_t seg = 0;
+        auto put = [&](const Rec &x) {
+            ok = seg < kRecords || wait_fast(bar(C::kRecEmpty + (seg % kRecords)), ((seg / kRecords) & 1) ^ 1, abort_flag);
+            if (!ok) return;
+            if (lane == 0) {
+                *reinterpret_cast<Rec *>(smem + C::OffRec + 64 * (seg % kRecords)) = x;
+                mbar_arrive(bar(C::kRecFull + (seg % kRecords)));
+            }
+            __syncwarp();
+            ++seg;
+        };
+        long left = count;
+        if (left > 0) {
+            int b = start[0];
+            long in = (long(start[3]) << 32) | uint32_t(start[2]);       // place in the sequence where the piece begins
+            for (; left > 0 && ok; ++b, in = 0) {
+                const Seq s = sequence<C>(p, b);
+                const long hc = head_cost<C>(s, group);
+                if (hc == 0) continue;
+                const int mts = row_tiles<C>(s, group);
+                long hd = in / hc;
+                in -= hd * hc;
+                for (; hd < heads && left > 0 && ok; ++hd) {
+                    for (int m = 0; m < mts && left > 0 && ok; ++m) {
+                        const long uc = unit_cost<C>(s, group, m);
+                        if (in >= uc) { in -= uc; continue; }
+                        // the unit's ends stand before its tiles; a tile is whose piece its beginning is in
+                        const int ut = int(unit_tiles<C>(s, group, m)), w = tile_cost<C>(s, group, m);
+                        auto tile_at = [&](long x) { return int(min(long(ut), max(0L, (x - C::kEnds + w - 1) / w))); };
+                        const long take = min(left, uc - in);
+                        Rec x{};
+                        x.t0 = tile_at(in);
+                        x.t1 = tile_at(in + take);
+                        if (x.t1 > x.t0) {
+                            x.l = int(hd / p.HK); x.b = b; x.hk = int(hd % p.HK); x.base = s.base; x.n = s.n; x.len = s.len;
+                            x.row0 = m * C::MT;
+                            x.rows = min(C::MT, s.n * group - x.row0);
+                            x.ct = s.ct;
+                            x.nodes = nodes_seen<C::MT>(s.n, group, m);
+                            x.slot = x.t0 == 0 && x.t1 == ut ? -1 : x.t0 == 0 ? 1 : 0;
+                            if (x.slot == 1) {
+                                // the unit ends in a later CTA's piece: where its last tile begins
+                                const long last = begin + (count - left) - in + C::kEnds + long(ut - 1) * w, wide = extra * (per + 1);
+                                const int owner = int(last < wide ? last / (per + 1) : extra + (last - wide) / per);
+                                join = Join{owner - cta + 1, x.l, x.hk, x.base, x.row0, x.rows, 0, 0};
+                            }
+                            put(x);
+                        }
+                        left -= take;
+                        in = 0;
+                    }
+                }
+            }
+        }
+        if (ok) put(Rec{});
+        if (lane == 0) {
+            if (!ok) join.parts = 0;
+            plan.join[cta] = join;
+        }
+    }
+};
+
+// the four maps of a call (a box of the cache is a page, or a tile's rows of one); 0 or an error
+template <int D> inline int encode_maps(const AttnParams &p, int box_rows, Maps &maps)
+{
+    EncodeTiledFn encode = encode_tiled_fn();
+    if (encode == nullptr) return int(cudaErrorNotSupported);
+    const int page = 1 << p.page_shift;
+    CUtensorMap *to[4] = {&maps.k, &maps.v, &maps.k_draft, &maps.v_draft};
+    const cuuint32_t es[5] = {1, 1, 1, 1, 1};
+    for (int i = 0; i < 4; ++i) {
+        const bool cache = i < 2;
+        const void *base = i == 0 ? p.k_cache : i == 1 ? p.v_cache : i == 2 ? p.k : p.v;
+        // 64 columns, eight rows, blocks of columns; of the cache groups of eight rows and (layer, page, head) besides, of the
+        // draft rows of all layers in place of the eight, and the head
+        const cuuint64_t row = cuuint64_t(D) * 2 * (cache ? 1 : p.HK);
+        const cuuint64_t dim[5] = {64, cache ? 8u : cuuint64_t(p.L) * p.T, D / 64, cuuint64_t(cache ? page / 8 : p.HK), cuuint64_t(p.L) * p.n_pages * p.HK};
+        const cuuint64_t stride[4] = {row, 128, cache ? 8 * row : cuuint64_t(D) * 2, cuuint64_t(page) * D * 2};
+        const cuuint32_t box[5] = {64, 8, D / 64, cuuint32_t(cache ? box_rows / 8 : 1), 1};
+        if (encode(to[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, cache ? 5 : 4, const_cast<void *>(base), dim, stride, box, es,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return int(cudaErrorInvalidValue);
+    }
+    return 0;
+}
+
+inline Plan make_plan(const AttnParams &p, int rows_cap, int d)
+{
+    Plan plan;
+    plan.rows_cap = rows_cap;
+    plan.slot_bytes = slot_bytes(rows_cap, d);
+    plan.join = static_cast<Join *>(p.workspace);
+    plan.slots = static_cast<char *>(p.workspace) + align256(sizeof(Join) * kMaxCtas);
+    return plan;
+}
+
+}  // namespace attend
+
+// few rows a unit (max_nodes * heads / kv_heads of them at most): rows of its tile, or 0
+int attend_few_rows(int d_head, long rows);
+int launch_attend_few(const AttnParams &p, int d_head, int rows, const attend::Maps &maps, const attend::Plan &plan, int box_rows, int grid,
+                      cudaStream_t st);
+
+}  // namespace speca
