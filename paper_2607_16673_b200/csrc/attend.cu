@@ -166,13 +166,15 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + C::OffMisc + 4);
     const int warp = x.warp, lane = x.lane, group = x.group, cta = blockIdx.x;
 
-    if (threadIdx.x == 0) {
+    if (warp == 0) {
         x.init(SOFT + 5, 1);
-        for (int i = 0; i < VS; ++i) mbar_init(bar(C::kVRaw + i), 1);
-        for (int i = 0; i < BUFS; ++i) { mbar_init(bar(C::kSFull + i), 1); mbar_init(bar(C::kPReady + i), 4); mbar_init(bar(C::kODone + i), 1); }
-        mbar_init(bar(C::kQFull), SOFT);
-        mbar_init(bar(C::kSync), SOFT);
-        mbar_init(bar(C::kDrain), 2);
+        if (lane < VS) mbar_init(bar(C::kVRaw + lane), 1);
+        if (lane < BUFS) { mbar_init(bar(C::kSFull + lane), 1); mbar_init(bar(C::kPReady + lane), 4); mbar_init(bar(C::kODone + lane), 1); }
+        if (lane == 0) {
+            mbar_init(bar(C::kQFull), SOFT);
+            mbar_init(bar(C::kSync), SOFT);
+            mbar_init(bar(C::kDrain), 2);
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == SOFT + 1) tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_slot)), kTmemCols);
@@ -642,7 +644,7 @@ join_kernel(AttnParams p, Plan plan, int32_t blocks)
 inline int unit_rows(int max_nodes, int group, int d)
 {
     const long rows = long(max_nodes) * group;
-    const int few = attend_few_rows(d, rows), mt = few > 0 ? few : d == 256 ? Cfg<256>::MT : Cfg<128>::MT;
+    const int few = attend_few_rows(rows), mt = few > 0 ? few : d == 256 ? Cfg<256>::MT : Cfg<128>::MT;
     return rows < mt ? int(rows) : mt;
 }
 
@@ -669,9 +671,8 @@ template <int D> int launch_width(const AttnParams &p, cudaStream_t st)
     const int rc = encode_maps<D>(p, box_rows, maps);
     if (rc != 0) return rc;
     const Plan plan = make_plan(p, unit_rows(p.max_nodes, p.H / p.HK, D), D);
-    const int few = attend_few_rows(D, long(p.max_nodes) * (p.H / p.HK));
-    if (few > 0) {
-        const int r = launch_attend_few(p, D, few, maps, plan, box_rows, grid, st);
+    if (attend_few_rows(long(p.max_nodes) * (p.H / p.HK)) > 0) {
+        const int r = launch_attend_few(p, D, maps, plan, box_rows, grid, st);
         if (r != 0) return r;
     } else launch(attend_kernel<D>, grid, C::THREADS, C::Bytes, st, maps, p, plan, int32_t(box_rows));
     const int e = int(cudaGetLastError());

@@ -142,6 +142,12 @@ template <class C> __device__ __forceinline__ long head_cost(const Seq &s, int g
 }
 
 
+// a / b of positive numbers: a division of 64 bits is a call of some hundred instructions, in front of the first tile
+__device__ __forceinline__ long quotient(long a, long b)
+{
+    return ((a | b) >> 31) == 0 ? long(uint32_t(a) / uint32_t(b)) : a / b;
+}
+
 struct Maps {
     CUtensorMap k, v, k_draft, v_draft;
 };
@@ -169,15 +175,14 @@ template <class C> struct Cta {
     {
     }
     __device__ __forceinline__ uint32_t bar(int i) const { return sbase + C::OffBars + 8u * uint32_t(i); }
-    // by one thread, before the barriers' fence
+    // by the first warp, before the barriers' fence
     __device__ __forceinline__ void init(int consumers, int empties)
     {
-        *abort_flag = 0;
-        topo_bad[0] = topo_bad[1] = 0;
-        for (int i = 0; i < 2 * kFlagRing; ++i) page_bad[i] = 0;
-        for (int i = 0; i < KS; ++i) { mbar_init(bar(C::kKFull + i), 1); mbar_init(bar(C::kKEmpty + i), empties); }
-        for (int i = 0; i < VS; ++i) { mbar_init(bar(C::kVFull + i), 1); mbar_init(bar(C::kVEmpty + i), empties); }
-        for (int i = 0; i < kRecords; ++i) { mbar_init(bar(C::kRecFull + i), 1); mbar_init(bar(C::kRecEmpty + i), consumers); }
+        if (lane == 0) *abort_flag = topo_bad[0] = topo_bad[1] = 0;
+        if (lane < 2 * kFlagRing) page_bad[lane] = 0;
+        if (lane < KS) { mbar_init(bar(C::kKFull + lane), 1); mbar_init(bar(C::kKEmpty + lane), empties); }
+        if (lane < VS) { mbar_init(bar(C::kVFull + lane), 1); mbar_init(bar(C::kVEmpty + lane), empties); }
+        if (lane < kRecords) { mbar_init(bar(C::kRecFull + lane), 1); mbar_init(bar(C::kRecEmpty + lane), consumers); }
     }
 
     // record of segment `s`; false: the list has ended, or (ok == false) the CTA is aborting
@@ -240,8 +245,8 @@ template <class C> struct Cta {
         before += incl - mine;
         // (a piece is at least one tile long, so that every CTA between a unit's first and last has some of it)
         const int pieces = int(min(long(grid), max(1L, total / (plan.rows_cap > 128 ? 2 : 1))));
-        per = total / pieces;
-        extra = total % pieces;
+        per = quotient(total, pieces);
+        extra = total - per * pieces;
         begin = cta * per + min(long(cta), extra);
         count = cta < pieces ? per + (cta < extra ? 1 : 0) : 0;
         if (count > 0 && begin >= before && begin < before + mine) {
@@ -342,7 +347,7 @@ template <class C> struct Cta {
                 const long hc = head_cost<C>(s, group);
                 if (hc == 0) continue;
                 const int mts = row_tiles<C>(s, group);
-                long hd = in / hc;
+                long hd = quotient(in, hc);
                 in -= hd * hc;
                 for (; hd < heads && left > 0 && ok; ++hd) {
                     for (int m = 0; m < mts && left > 0 && ok; ++m) {
@@ -356,7 +361,7 @@ template <class C> struct Cta {
                         x.t0 = tile_at(in);
                         x.t1 = tile_at(in + take);
                         if (x.t1 > x.t0) {
-                            x.l = int(hd / p.HK); x.b = b; x.hk = int(hd % p.HK); x.base = s.base; x.n = s.n; x.len = s.len;
+                            x.l = int(hd) / p.HK; x.b = b; x.hk = int(hd) - x.l * p.HK; x.base = s.base; x.n = s.n; x.len = s.len;
                             x.row0 = m * C::MT;
                             x.rows = min(C::MT, s.n * group - x.row0);
                             x.ct = s.ct;
@@ -365,7 +370,7 @@ template <class C> struct Cta {
                             if (x.slot == 1) {
                                 // the unit ends in a later CTA's piece: where its last tile begins
                                 const long last = begin + (count - left) - in + C::kEnds + long(ut - 1) * w, wide = extra * (per + 1);
-                                const int owner = int(last < wide ? last / (per + 1) : extra + (last - wide) / per);
+                                const int owner = int(last < wide ? quotient(last, per + 1) : extra + quotient(last - wide, per));
                                 join = Join{owner - cta + 1, x.l, x.hk, x.base, x.row0, x.rows, 0, 0};
                             }
                             put(x);
@@ -422,8 +427,8 @@ inline Plan make_plan(const AttnParams &p, int rows_cap, int d)
 }  // namespace attend
 
 // few rows a unit (max_nodes * heads / kv_heads of them at most): rows of its tile, or 0
-int attend_few_rows(int d_head, long rows);
-int launch_attend_few(const AttnParams &p, int d_head, int rows, const attend::Maps &maps, const attend::Plan &plan, int box_rows, int grid,
+int attend_few_rows(long rows);
+int launch_attend_few(const AttnParams &p, int d_head, const attend::Maps &maps, const attend::Plan &plan, int box_rows, int grid,
                       cudaStream_t st);
 
 }  // namespace speca

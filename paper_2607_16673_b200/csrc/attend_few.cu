@@ -1,12 +1,13 @@
 // Verification by an attention layer where a key head has few rows: single tokens, short chains, small trees.
 //
 // The 128-row products of the other kernel would be padding for the most part; it is fast enough for the bytes all the same,
-// but 64 single tokens over long contexts then run into the power limit (1000 W, 1.55 GHz) and a single chain waits for TMEM,
-// products and softmax in turn.  Here eight warps share a tile: each has 16 rows, 16 to 64 of the tile's keys and up to 128
-// columns of O, with a maximum and sums of its own, and warp-level products (m16n8k16) whose operands come out of the same
-// swizzled tiles by ldmatrix.  S stays in registers, where it becomes P.  Nothing is exchanged before a unit's end.
-#include <type_traits>
-
+// but 64 single tokens over long contexts then run into the power limit (1000 W, 1.55 GHz; 441 us against 369 here) and a
+// single chain waits for TMEM, products and softmax in turn.  Here eight warps share a tile: each has the 16 rows, an
+// eighth of the tile's keys and all columns of O (D <= 128; a quarter and half of them at 256), with a maximum and sums of its own, and warp-level products (m16n8k16) whose
+// operands come out of the same swizzled tiles by ldmatrix.  S stays in registers, where it becomes P.  Nothing is exchanged
+// before a unit's end, where 64 columns of all warps fit into shared memory together (32 columns at a time the end took four
+// more barriers and half as long again).  A warp has 128 columns: with 64, every score is formed by twice as many warps, and 64
+// single tokens over long contexts took 398 us, not 363.
 #include "attend_common.cuh"
 
 namespace speca {
@@ -16,34 +17,35 @@ using namespace attend;
 namespace {
 
 constexpr int kConsumers = 8;            // warps that compute; then keys, schedule, values
+constexpr int kRows = 16;
 constexpr float kSlack = 8.f;            // binary digits a maximum may grow by before O is scaled
-constexpr int kStageRow = 36;            // floats from row to row where warps add up their sums: 32 columns and some to spread banks
 
-// RB blocks of 16 rows.  A warp has one of them, KW of the tile's N keys and OC columns.
-template <int DH, int RB> struct Few {
+// A warp has KW of the tile's N keys and OC columns.
+template <int DH> struct Few {
     static constexpr int D = DH;
     static constexpr int N = D == 256 ? 64 : 128;
-    static constexpr int LANES = 1, MT = 16 * RB, kEnds = 1;
+    static constexpr int LANES = 1, MT = kRows, kEnds = 3;
     static constexpr bool kMend = false;
     static constexpr int THREADS = (kConsumers + 3) * 32;
     static constexpr int OC = D < 128 ? D : 128, CH = D / OC;
-    static constexpr int KB = kConsumers / (RB * CH), KW = N / KB;
+    static constexpr int KB = kConsumers / CH, KW = N / KB;
     static constexpr int TILE = N * D * 2;
     static constexpr int KS = D == 64 ? 6 : 3, VS = KS;
-    static constexpr int kStage = kConsumers * 16 * kStageRow * 4;
     static constexpr int OffRing = 0;
-    static constexpr int OffQ = (KS + VS) * TILE;            // queries; at a unit's end sums on their way
-    static constexpr int OffPar = OffQ + (MT * D * 2 > kStage ? MT * D * 2 : kStage);        // scratch of the scan, then int16 parent[MT]
-    static constexpr int OffMl = OffPar + 256;               // float2 [warp][16]
-    static constexpr int OffRec = OffMl + kConsumers * 16 * 8;
+    static constexpr int OffQ = (KS + VS) * TILE;            // queries; at a unit's end the warps' sums, float [warp][row][64]
+    static constexpr int OffPar = OffQ + kConsumers * kRows * 64 * 4;        // scratch of the scan, then int16 parent[kRows]
+    static constexpr int OffMl = OffPar + 128;               // float2 [warp][row]
+    static constexpr int OffRec = OffMl + kConsumers * kRows * 8;
     static constexpr int OffBars = OffRec + 64 * kRecords;
     static constexpr int kKFull = 0, kKEmpty = KS, kVFull = 2 * KS, kVEmpty = kVFull + VS, kVRaw = 0, kSync = kVEmpty + VS, kRecFull = kSync + 1,
                          kRecEmpty = kRecFull + kRecords, kBars = kRecEmpty + kRecords;
     static constexpr int OffMisc = OffBars + 8 * kBars;
     static constexpr int OffFlags = OffMisc + 64;
     static constexpr int Bytes = OffFlags + 8 * kFlagRing;
-    static_assert(KW % 16 == 0 && KB * KW == N && OffQ % 1024 == 0 && Bytes <= 232448, "layout");
+    static_assert(KW % 16 == 0 && KB * KW == N && OffQ % 1024 == 0 && kRows * D * 2 <= kConsumers * kRows * 64 * 4 && Bytes <= 232448, "layout");
 };
+// four sums of a row, spread over the banks
+__device__ __forceinline__ int stage_offset(int warp, int row, int col) { return (warp * kRows + row) * 64 + (col ^ ((row & 7) << 3)); }
 
 __device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t (&x)[4])
 {
@@ -70,12 +72,12 @@ __device__ __forceinline__ bool strip(uint32_t &pair)
     return lo || hi;
 }
 
-template <int D, int RB>
-__global__ void __launch_bounds__(Few<D, RB>::THREADS, 1)
+template <int D>
+__global__ void __launch_bounds__(Few<D>::THREADS, 1)
 attend_few_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_t box_rows)
 {
     after_previous_kernel();
-    using C = Few<D, RB>;
+    using C = Few<D>;
     constexpr int KB = C::KB, KW = C::KW, OC = C::OC, KS = C::KS, VS = C::VS;
     extern __shared__ __align__(1024) uint8_t smem[];
     Cta<C> x(p, plan, smem);
@@ -84,9 +86,9 @@ attend_few_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, in
         return;
     }
     const int warp = x.warp, lane = x.lane, group = x.group, cta = blockIdx.x;
-    if (threadIdx.x == 0) {
+    if (warp == 0) {
         x.init(kConsumers + 2, kConsumers);
-        mbar_init(x.bar(C::kSync), kConsumers);
+        if (lane == 0) mbar_init(x.bar(C::kSync), kConsumers);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     x.find_piece();
@@ -95,7 +97,7 @@ attend_few_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, in
     else if (warp == kConsumers + 2) x.template load<1>(maps, box_rows);
     else if (warp == kConsumers + 1) x.schedule();
     else {
-        const int kb = warp % KB, ch = warp / KB % C::CH, rb = warp / (KB * C::CH);
+        const int kb = warp % KB, ch = warp / KB;
         const int k0 = kb * KW;                              // this warp's first key of a tile
         const float c2 = p.scale * 1.4426950408889634f;
         const uint32_t q_at = x.sbase + C::OffQ;
@@ -131,15 +133,15 @@ attend_few_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, in
             }
             copy16_wait();
             if (!(x.ok = sync())) break;
-            // this lane's rows of the unit: lane / 4 of its block, and eight further
-            const int row0 = rb * 16 + (lane >> 2);
-            uint64_t seen[2] = {0u, 0u};                     // draft nodes they attend
+            // this lane's rows of the unit, and the draft nodes they attend (no more nodes than rows)
+            const int row0 = lane >> 2;
+            uint32_t seen[2] = {0u, 0u};
             bool live[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 live[h] = row0 + 8 * h < r.rows;
                 if (!live[h] || r.t1 <= r.ct) continue;
-                for (int a = (r.row0 + row0 + 8 * h) / group; a >= 0; a = tree ? int(par[a]) : a - 1) seen[h] |= 1ull << a;
+                for (int a = (r.row0 + row0 + 8 * h) / group; a >= 0; a = tree ? int(par[a]) : a - 1) seen[h] |= 1u << a;
             }
             float o[OC / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
@@ -164,7 +166,7 @@ attend_few_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, in
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k) {
                         uint32_t a[4];
-                        ldmatrix4(q_at + tile_offset<D>(rb * 16 + (lane & 15), 2 * k + (lane >> 4)), a);
+                        ldmatrix4(q_at + tile_offset<D>(lane & 15, 2 * k + (lane >> 4)), a);
 #pragma unroll
                         for (int j = 0; j < KW / 16; ++j) {
                             uint32_t b[4];
@@ -184,7 +186,7 @@ attend_few_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, in
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
                                 const int key = k0 + 8 * j + (lane & 3) * 2 + (e & 1);
-                                if (key >= valid || (draft && !(seen[e >> 1] >> (key & 63) & 1u))) s[j][e] = -INFINITY;
+                                if (key >= valid || (draft && !(seen[e >> 1] >> (key & 31) & 1u))) s[j][e] = -INFINITY;
                             }
                     }
                     float top[2] = {-INFINITY, -INFINITY};
@@ -265,9 +267,9 @@ attend_few_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, in
             for (int h = 0; h < 2; ++h) {
                 l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
                 l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-                if ((lane & 3) == 0) ml[warp * 16 + (lane >> 2) + 8 * h] = make_float2(m[h], l[h]);
+                if ((lane & 3) == 0) ml[warp * kRows + row0 + 8 * h] = make_float2(m[h], l[h]);
             }
-            if (!(x.ok = sync())) break;
+            if (!(x.ok = sync())) break;                     // (the queries have been used by all)
             const bool skip = (x.topo_bad[seg & 1] != 0 && tree) || x.page_bad[seg % kFlagRing] == int(seg) + 1;
             const bool put_back = x.value_bad[seg % kFlagRing] == int(seg) + 1;
             float *sums = r.slot >= 0 ? slot_sums(plan, cta, r.slot) : nullptr;
@@ -275,51 +277,46 @@ attend_few_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, in
                 const int at = r.row0 + row, node = at / group, g = at - node * group;
                 return p.o + ((size_t(r.l) * p.T + r.base + node) * p.H + r.hk * group + g) * D;
             };
-            float f[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float2 *all = ml + (warp - kb) * 16 + (lane >> 2) + 8 * h;
-                float mm = -INFINITY, ll = 0.f;
-#pragma unroll
-                for (int i = 0; i < KB; ++i) mm = fmaxf(mm, all[16 * i].x);
-#pragma unroll
-                for (int i = 0; i < KB; ++i) {
-                    const float2 y = all[16 * i];
-                    ll += y.y * (y.x == mm || y.y == 0.f ? 1.f : exp2_approx((y.x - mm) * c2));
-                }
-                f[h] = m[h] == mm || m[h] == -INFINITY ? 1.f : exp2_approx((m[h] - mm) * c2);
-                if (sums == nullptr) f[h] *= 1.f / ll;
-                else if (kb == 0 && ch == 0 && (lane & 3) == 0 && live[h] && !skip)
-                    reinterpret_cast<float2 *>(sums + size_t(plan.rows_cap) * D)[row0 + 8 * h] = make_float2(mm, ll);
-            }
             if (sums != nullptr && threadIdx.x == 0) reinterpret_cast<int *>(sums + size_t(plan.rows_cap) * (D + 2))[0] = skip;
 #pragma unroll
-            for (int c = 0; c < OC / 32; ++c) {
+            for (int turn = 0; turn < OC / 64; ++turn) {
+                if (turn > 0 && !(x.ok = sync())) break;
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
+                for (int j = 0; j < 8; ++j)
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
-                        *reinterpret_cast<float2 *>(stage + (warp * 16 + (lane >> 2) + 8 * h) * kStageRow + 8 * j + (lane & 3) * 2) =
-                            make_float2(o[4 * c + j][2 * h] * f[h], o[4 * c + j][2 * h + 1] * f[h]);
+                        *reinterpret_cast<float2 *>(stage + stage_offset(warp, row0 + 8 * h, 8 * j + (lane & 3) * 2)) =
+                            make_float2(o[8 * turn + j][2 * h], o[8 * turn + j][2 * h + 1]);
                 if (!(x.ok = sync())) break;
-                // four columns of a row a thread
+                // four columns of a row a thread, of the 64 that each group of warps has put there
 #pragma unroll 1
-                for (int u = threadIdx.x; u < RB * C::CH * 128; u += kConsumers * 32) {
-                    const int gi = u >> 7, rr = u >> 3 & 15, e = (u & 7) * 4, row = gi / C::CH * 16 + rr;
-                    if (row >= r.rows || skip) continue;
+                for (int u = threadIdx.x; u < r.rows * (C::CH * 16) && !skip; u += kConsumers * 32) {
+                    const int row = u / (C::CH * 16), part = u / 16 % C::CH, e = u % 16 * 4, first = part * KB, col = part * OC + 64 * turn + e;
+                    float mm = -INFINITY, ll = 0.f;
+#pragma unroll
+                    for (int i = 0; i < KB; ++i) mm = fmaxf(mm, ml[(first + i) * kRows + row].x);
                     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                     for (int i = 0; i < KB; ++i) {
-                        const float4 y = *reinterpret_cast<const float4 *>(stage + ((gi * KB + i) * 16 + rr) * kStageRow + e);
-                        sum.x += y.x; sum.y += y.y; sum.z += y.z; sum.w += y.w;
+                        const float2 w = ml[(first + i) * kRows + row];
+                        // (a warp without a key of this row has zeros)
+                        const float f = w.x == mm || w.x == -INFINITY ? 1.f : exp2_approx((w.x - mm) * c2);
+                        const float4 y = *reinterpret_cast<const float4 *>(stage + stage_offset(first + i, row, e));
+                        ll = fmaf(w.y, f, ll);
+                        sum.x = fmaf(y.x, f, sum.x); sum.y = fmaf(y.y, f, sum.y); sum.z = fmaf(y.z, f, sum.z); sum.w = fmaf(y.w, f, sum.w);
                     }
-                    const int col = gi % C::CH * OC + 32 * c + e;
-                    if (sums == nullptr)
-                        *reinterpret_cast<uint2 *>(out_of(row) + col) = make_uint2(pack_bf16(sum.x, sum.y), pack_bf16(sum.z, sum.w));
-                    else *reinterpret_cast<float4 *>(sums + size_t(row) * D + col) = sum;
+                    if (sums == nullptr) {
+                        const float inv = 1.f / ll;
+                        *reinterpret_cast<uint2 *>(out_of(row) + col) = make_uint2(pack_bf16(sum.x * inv, sum.y * inv), pack_bf16(sum.z * inv, sum.w * inv));
+                    } else {
+                        *reinterpret_cast<float4 *>(sums + size_t(row) * D + col) = sum;
+                        if (col == 0) reinterpret_cast<float2 *>(sums + size_t(plan.rows_cap) * D)[row] = make_float2(mm, ll);
+                    }
                 }
-                if (!(x.ok = sync())) break;
             }
+            if (!x.ok) break;
+            // (what other threads wrote is read back)
+            if (put_back && !skip && !(x.ok = sync())) break;
             if (x.ok && put_back && !skip)
                 for (int u = threadIdx.x; u < r.rows * D; u += kConsumers * 32) {
                     // (column u % D of a row; what other threads have written of it is behind the last sync)
@@ -347,23 +344,20 @@ attend_few_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, in
 
 std::atomic<bool> g_opted_in[64];                            // per device: shared memory of every instantiation
 
-template <int D, int RB>
-int launch_few(const AttnParams &p, const Maps &maps, const Plan &plan, int box_rows, int grid, cudaStream_t st)
+template <int D> int launch_few(const AttnParams &p, const Maps &maps, const Plan &plan, int box_rows, int grid, cudaStream_t st)
 {
-    using C = Few<D, RB>;
-    launch(attend_few_kernel<D, RB>, unsigned(grid), C::THREADS, C::Bytes, st, maps, p, plan, int32_t(box_rows));
+    using C = Few<D>;
+    launch(attend_few_kernel<D>, unsigned(grid), C::THREADS, C::Bytes, st, maps, p, plan, int32_t(box_rows));
     return int(cudaGetLastError());
 }
 
 }  // namespace
 
-int attend_few_rows(int d_head, long rows)
-{
-    (void)d_head;
-    return rows <= 16 ? 16 : 0;
-}
+// A chain of n tokens, 32 sequences over 500..8000 tokens, 32 heads over 8 of 128 columns, this kernel / the other one: 4 rows 97 /
+// 104 us, 16 rows 102 / 106; of two blocks of 16 rows 156 / 107, of four 273 / 116.
+int attend_few_rows(long rows) { return rows <= kRows ? kRows : 0; }
 
-int launch_attend_few(const AttnParams &p, int d_head, int rows, const Maps &maps, const Plan &plan, int box_rows, int grid, cudaStream_t st)
+int launch_attend_few(const AttnParams &p, int d_head, const Maps &maps, const Plan &plan, int box_rows, int grid, cudaStream_t st)
 {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return int(cudaErrorInvalidDevice);
@@ -372,26 +366,15 @@ int launch_attend_few(const AttnParams &p, int d_head, int rows, const Maps &map
         auto opt_in = [&](const void *k, int bytes) {
             if (e == cudaSuccess) e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
         };
-        opt_in(reinterpret_cast<const void *>(attend_few_kernel<64, 1>), Few<64, 1>::Bytes);
-        opt_in(reinterpret_cast<const void *>(attend_few_kernel<64, 2>), Few<64, 2>::Bytes);
-        opt_in(reinterpret_cast<const void *>(attend_few_kernel<64, 4>), Few<64, 4>::Bytes);
-        opt_in(reinterpret_cast<const void *>(attend_few_kernel<128, 1>), Few<128, 1>::Bytes);
-        opt_in(reinterpret_cast<const void *>(attend_few_kernel<128, 2>), Few<128, 2>::Bytes);
-        opt_in(reinterpret_cast<const void *>(attend_few_kernel<128, 4>), Few<128, 4>::Bytes);
-        opt_in(reinterpret_cast<const void *>(attend_few_kernel<256, 1>), Few<256, 1>::Bytes);
-        opt_in(reinterpret_cast<const void *>(attend_few_kernel<256, 2>), Few<256, 2>::Bytes);
-        opt_in(reinterpret_cast<const void *>(attend_few_kernel<256, 4>), Few<256, 4>::Bytes);
+        opt_in(reinterpret_cast<const void *>(attend_few_kernel<64>), Few<64>::Bytes);
+        opt_in(reinterpret_cast<const void *>(attend_few_kernel<128>), Few<128>::Bytes);
+        opt_in(reinterpret_cast<const void *>(attend_few_kernel<256>), Few<256>::Bytes);
         if (e != cudaSuccess) return int(e);
         g_opted_in[dev].store(true, std::memory_order_release);
     }
-    auto width = [&](auto d) {
-        constexpr int D = decltype(d)::value;
-        return rows == 16 ? launch_few<D, 1>(p, maps, plan, box_rows, grid, st) : rows == 32 ? launch_few<D, 2>(p, maps, plan, box_rows, grid, st)
-                                                                                            : launch_few<D, 4>(p, maps, plan, box_rows, grid, st);
-    };
-    if (d_head == 64) return width(std::integral_constant<int, 64>{});
-    if (d_head == 128) return width(std::integral_constant<int, 128>{});
-    return width(std::integral_constant<int, 256>{});
+    if (d_head == 64) return launch_few<64>(p, maps, plan, box_rows, grid, st);
+    if (d_head == 128) return launch_few<128>(p, maps, plan, box_rows, grid, st);
+    return launch_few<256>(p, maps, plan, box_rows, grid, st);
 }
 
 }  // namespace speca
