@@ -40,13 +40,13 @@ template <int DH> struct Cfg {
     static constexpr int KS = D == 64 ? 5 : 2, VS = D == 64 ? 5 : 3;       // tiles of keys and of values in flight or in use
     static constexpr int OffQ = 0;
     static constexpr int OffRing = LANES * Q_BYTES;
-    static constexpr int OffPar = OffRing + (KS + VS) * TILE;    // int16 parent[kAttnMaxTree]; scratch of the scan before that
+    static constexpr int OffPar = OffRing + (KS + VS) * TILE;    // int16 parent[kAttnMaxTree]
     static constexpr int OffRec = OffPar + 2 * kAttnMaxTree;
     static constexpr int OffBars = OffRec + 64 * kRecords;
     static constexpr int kKFull = 0, kKEmpty = KS, kVFull = 2 * KS, kVEmpty = kVFull + VS, kVRaw = kVEmpty + VS, kSFull = kVRaw + VS, kPReady = kSFull + BUFS, kODone = kPReady + BUFS,
-                         kQFull = kODone + BUFS, kSync = kQFull + 1, kRecFull = kSync + 1, kRecEmpty = kRecFull + kRecords,
+                         kQFull = kODone + BUFS, kRecFull = kQFull + 1, kRecEmpty = kRecFull + kRecords,
                          kDrain = kRecEmpty + kRecords, kBars = kDrain + 1;
-    static constexpr int OffMisc = OffBars + 8 * kBars;      // abort, TMEM base, bad topology [2], start of the piece [4]
+    static constexpr int OffMisc = OffBars + 8 * kBars;      // abort, TMEM base, bad topology [2]
     static constexpr int OffFlags = OffMisc + 64;            // segment numbers: bad page [8], values that are not finite [8]
     static constexpr int Bytes = OffFlags + 8 * kFlagRing;
 };
@@ -172,14 +172,13 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
         if (lane < BUFS) { mbar_init(bar(C::kSFull + lane), 1); mbar_init(bar(C::kPReady + lane), 4); mbar_init(bar(C::kODone + lane), 1); }
         if (lane == 0) {
             mbar_init(bar(C::kQFull), SOFT);
-            mbar_init(bar(C::kSync), SOFT);
             mbar_init(bar(C::kDrain), 2);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == SOFT + 1) tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_slot)), kTmemCols);
 
-    x.find_piece();
+    x.begin();
     const uint32_t tmem = *tmem_slot, lead = x.lead;
     bool &ok = x.ok;
     auto record = [&](uint32_t s, Rec &r) { return x.record(s, r); };
@@ -302,19 +301,15 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
         const int wg = warp >> 2, quad = warp & 3, trow = quad * 32 + lane;      // lane of TMEM: row of this group's tile
         const uint32_t tq = tmem + (uint32_t(quad * 32) << 16);
         const float c2 = p.scale * 1.4426950408889634f;
-        uint32_t syncs = 0, phase = 0;
+        uint32_t phase = 0;
         int16_t *par = reinterpret_cast<int16_t *>(smem + C::OffPar);
-        auto sync = [&]() -> bool {
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(C::kSync));
-            return wait_fast(bar(C::kSync), syncs++ & 1, abort_flag);
-        };
-        for (uint32_t seg = 0; ok && record(seg, r); ++seg) {
+        auto sync = [&]() { return ok = all_well<SOFT * 32>(ok); };
+        for (uint32_t seg = 0;; ++seg) {
+            const bool more = record(seg, r);
+            if (!sync() || !more) break;                     // everyone is through with the last segment: its queries, its parents
             const bool two = LANES == 2 && r.rows > 128;
             const int tiles = r.t1 - r.t0;
             const int all = tiles << (two ? 1 : 0);          // items of both groups
-            // everyone is through with the last segment: its queries, its parents, its sums
-            if (!(ok = sync())) break;
             if (threadIdx.x == 0) topo_bad[(seg & 1) ^ 1] = 0;
             {
                 const int chunks = r.rows * (D / 8);
@@ -340,7 +335,7 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
                     topo_bad[seg & 1] = 1;
                     atomicOr(p.status, SPECA_STATUS_BAD_PARENT);
                 }
-                if (!(ok = sync())) break;
+                if (!sync()) break;
             }
             const int row = (two ? wg * 128 : 0) + trow;     // row of the unit
             const bool live = (two ? wg * 128 : 0) + quad * 32 < r.rows;     // the warp has rows
@@ -457,14 +452,14 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(C::kPReady + buf));
             }
-            if (!ok) break;
 
             // ---- end of the segment: this group's last product covers those before it
             const bool merge = LANES == 2 && !two;
-            if (mine > 0) {
+            if (mine > 0 && ok) {
                 const int last = buffer(LANES == 2 ? 2 * (mine - 1) + wg : mine - 1);
-                if (!(ok = wait_fast(bar(C::kODone + last), ((uses >> last) & 1) ^ 1, abort_flag))) break;
+                ok = wait_fast(bar(C::kODone + last), ((uses >> last) & 1) ^ 1, abort_flag);
             }
+            if (!ok) { sync(); break; }
 #pragma unroll
             for (int b = 0; b < BUFS; ++b) phase ^= uint32_t((all + BUFS - 1 - b) / BUFS & 1) << b;      // items of all groups in buffer b
             tc_fence_after();
@@ -475,7 +470,7 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
                 tmem_st2(tq + wg * N, m, l);
                 tmem_st_wait();
                 tc_fence_before();
-                if (!(ok = sync())) break;
+                if (!sync()) break;
                 tc_fence_after();
                 float2 a, b;
                 tmem_ld2(tq, a);
@@ -610,29 +605,54 @@ join_kernel(AttnParams p, Plan plan, int32_t blocks)
     const int row = (blockIdx.x % blocks) * kJoinWarps + (threadIdx.x >> 5);
     if (j.parts <= 1 || row >= j.rows) return;
     const float c2 = p.scale * 1.4426950408889634f;
-    auto tail = [&](int i) { return slot_sums(plan, cta + i, i == 0 ? 1 : 0) + size_t(plan.rows_cap) * D; };
-    float m = -INFINITY;
+    constexpr int E = D / 32, AT_ONCE = 8;
+    auto part = [&](int i) { return slot_sums(plan, cta + i, i == 0 ? 1 : 0); };
+    float o[E], l = 0.f, m = -INFINITY;
     int skip = 0;
-    for (int i = lane; i < j.parts; i += 32) {
-        m = fmaxf(m, reinterpret_cast<const float2 *>(tail(i))[row].x);
-        skip |= reinterpret_cast<const int *>(tail(i) + 2 * plan.rows_cap)[0];
-    }
-#pragma unroll
-    for (int w = 16; w > 0; w /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
-    if (__any_sync(0xffffffffu, skip)) return;
-    constexpr int E = D / 32;
-    float o[E], l = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = 0.f;
-#pragma unroll 2
-    for (int i = 0; i < j.parts; ++i) {
-        const float2 ml = reinterpret_cast<const float2 *>(tail(i))[row];
-        const float f = ml.x == m ? 1.f : exp2_approx((ml.x - m) * c2);
-        const float *x = slot_sums(plan, cta + i, i == 0 ? 1 : 0) + size_t(row) * D + lane * E;
-        l = fmaf(ml.y, f, l);
+    // eight parts at a time, their sums asked for together with their maxima (one round trip each)
+#pragma unroll 1
+    for (int i0 = 0; i0 < j.parts; i0 += AT_ONCE) {
+        float2 ml = make_float2(-INFINITY, 0.f);
+        float x[AT_ONCE][E];
+        if (lane < AT_ONCE && i0 + lane < j.parts) {
+            const float *tail = part(i0 + lane) + size_t(plan.rows_cap) * D;
+            ml = reinterpret_cast<const float2 *>(tail)[row];
+            skip |= reinterpret_cast<const int *>(tail + 2 * plan.rows_cap)[0];
+        }
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = fmaf(x[e], f, o[e]);
+        for (int i = 0; i < AT_ONCE; ++i) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[i][e] = 0.f;
+            if (i0 + i < j.parts) {
+                const float *at = part(i0 + i) + size_t(row) * D + lane * E;
+                if constexpr (E == 2) *reinterpret_cast<float2 *>(x[i]) = *reinterpret_cast<const float2 *>(at);
+                else
+#pragma unroll
+                    for (int e = 0; e < E; e += 4) *reinterpret_cast<float4 *>(x[i] + e) = *reinterpret_cast<const float4 *>(at + e);
+            }
+        }
+        float top = ml.x;
+#pragma unroll
+        for (int w = AT_ONCE / 2; w > 0; w /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+        top = fmaxf(m, __shfl_sync(0xffffffffu, top, 0));
+        // (what has nothing yet is zero in whatever scale)
+        const float old = m == top || m == -INFINITY ? 1.f : exp2_approx((m - top) * c2);
+        const float mine = ml.x == top || ml.x == -INFINITY ? 1.f : exp2_approx((ml.x - top) * c2);
+        m = top;
+        l *= old;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] *= old;
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const float f = __shfl_sync(0xffffffffu, mine, i);
+            l = fmaf(__shfl_sync(0xffffffffu, ml.y, i), f, l);
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = fmaf(x[i][e], f, o[e]);
+        }
     }
+    if (__any_sync(0xffffffffu, skip)) return;
     const int group = p.H / p.HK, at = j.row0 + row, node = at / group, g = at % group;
     __nv_bfloat16 *to = p.o + ((size_t(j.l) * p.T + j.base + node) * p.H + j.hk * group + g) * D + lane * E;
     const float inv = 1.f / l;

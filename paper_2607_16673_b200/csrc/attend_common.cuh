@@ -164,7 +164,6 @@ template <class C> struct Cta {
     uint32_t sbase;
     int warp, lane, group;
     volatile int *abort_flag, *topo_bad, *page_bad, *value_bad;      // topo_bad [2], the others [kFlagRing]: 1 + segment number
-    long begin, count, per, extra;                           // this CTA's piece of the list
     uint32_t lead;
     bool ok;
 
@@ -212,56 +211,12 @@ template <class C> struct Cta {
         return C::kMend && ((valid_of(r, t) & 15) != 0 || !all_seen(r, t));
     }
 
-    // Cost of the whole list, and this CTA's piece; whole CTA.
-    __device__ __forceinline__ void find_piece()
+    // barriers and flags are set up; whole CTA
+    __device__ __forceinline__ void begin()
     {
-        const int grid = gridDim.x, cta = blockIdx.x;
-        volatile int *start = abort_flag + 4;                // sequence, then place in it (64 bits)
-        // ---- cost of the whole list, and where this CTA's piece begins: every thread has some consecutive sequences
-        long mine = 0, before = 0, total = 0;
-        const int per_thread = (p.B + C::THREADS - 1) / C::THREADS;
-        const int b_lo = min(p.B, int(threadIdx.x) * per_thread), b_hi = min(p.B, b_lo + per_thread);
-        const long heads = long(p.L) * p.HK;
-        for (int b = b_lo; b < b_hi; ++b) {
-            const Seq s = sequence<C>(p, b);
-            if (s.fault && cta == 0) atomicOr(p.status, s.fault);
-            mine += heads * head_cost<C>(s, group);
-        }
-        long incl = mine;
-#pragma unroll
-        for (int i = 1; i < 32; i *= 2) {
-            const long x = __shfl_up_sync(0xffffffffu, incl, i);
-            if (lane >= i) incl += x;
-        }
-        volatile long *sums = reinterpret_cast<volatile long *>(smem + C::OffPar);
-        if (lane == 31) sums[warp] = incl;
         tc_fence_before();
         __syncthreads();
         tc_fence_after();
-        for (int w = 0; w < C::THREADS / 32; ++w) {
-            if (w < warp) before += sums[w];
-            total += sums[w];
-        }
-        before += incl - mine;
-        // (a piece is at least one tile long, so that every CTA between a unit's first and last has some of it)
-        const int pieces = int(min(long(grid), max(1L, total / (plan.rows_cap > 128 ? 2 : 1))));
-        per = quotient(total, pieces);
-        extra = total - per * pieces;
-        begin = cta * per + min(long(cta), extra);
-        count = cta < pieces ? per + (cta < extra ? 1 : 0) : 0;
-        if (count > 0 && begin >= before && begin < before + mine) {
-            long rem = begin - before;
-            int b = b_lo;
-            for (;; ++b) {
-                const long t = heads * head_cost<C>(sequence<C>(p, b), group);
-                if (rem < t) break;
-                rem -= t;
-            }
-            start[0] = b;
-            start[2] = int(rem & 0xffffffffL);
-            start[3] = int(rem >> 32);
-        }
-        __syncthreads();
         lead = elect_one();
     }
 
@@ -320,12 +275,13 @@ template <class C> struct Cta {
         }
     }
 
-    // Records of the piece, one warp, and what the join needs of it.
+    // Cost of the whole list, this CTA's piece of it, its records and what the join needs of it; one warp, the others only wait for
+    // its first record (with all of them adding up sequences and two barriers it came 1.5 us later, most of it instructions
+    // fetched for the first time).
     __device__ __forceinline__ void schedule()
     {
-        const int cta = blockIdx.x;
-        const long heads = long(p.L) * p.HK;
-        volatile int *start = abort_flag + 4;
+        const int grid = gridDim.x, cta = blockIdx.x;
+        const int heads = p.L * p.HK;
         Join join{0, 0, 0, 0, 0, 0, 0, 0};
         uint32_t seg = 0;
         auto put = [&](const Rec &x) {
@@ -338,47 +294,86 @@ template <class C> struct Cta {
             __syncwarp();
             ++seg;
         };
-        long left = count;
-        if (left > 0) {
-            int b = start[0];
-            long in = (long(start[3]) << 32) | uint32_t(start[2]);       // place in the sequence where the piece begins
-            for (; left > 0 && ok; ++b, in = 0) {
-                const Seq s = sequence<C>(p, b);
-                const long hc = head_cost<C>(s, group);
+        // 32 sequences at a time, one a lane: the cost of one layer and key head of each
+        Seq s{};
+        auto fetch = [&](int b0) {
+            s = Seq{0, 0, 0, 0, 0};
+            if (b0 + lane >= p.B) return 0L;
+            s = sequence<C>(p, b0 + lane);
+            return head_cost<C>(s, group);
+        };
+        long total = 0, first = 0;
+#pragma unroll 1
+        for (int b0 = 0; b0 < p.B; b0 += 32) {
+            const long c = fetch(b0);
+            if (b0 == 0) first = c;
+            if (s.fault && cta == 0) atomicOr(p.status, s.fault);
+            total += c;
+        }
+#pragma unroll
+        for (int i = 16; i > 0; i /= 2) total += __shfl_xor_sync(0xffffffffu, total, i);
+        total *= heads;
+        // (a piece is at least one tile long, so that every CTA between a unit's first and last has some of it)
+        const int pieces = int(min(long(grid), max(1L, total / (plan.rows_cap > 128 ? 2 : 1))));
+        const long per = quotient(total, pieces), extra = total - per * pieces;
+        const long begin = cta * per + min(long(cta), extra), end = cta < pieces ? begin + per + (cta < extra ? 1 : 0) : begin;
+        long at = 0;                                         // place in the list of the sequence looked at
+#pragma unroll 1
+        for (int b0 = 0; b0 < p.B && at < end && ok; b0 += 32) {
+            const long mine = p.B <= 32 ? first : fetch(b0);
+            long upto = mine * heads;                        // to the end of this lane's sequence, from the first of the 32
+#pragma unroll
+            for (int i = 1; i < 32; i *= 2) {
+                const long y = __shfl_up_sync(0xffffffffu, upto, i);
+                if (lane >= i) upto += y;
+            }
+            const uint32_t later = __ballot_sync(0xffffffffu, at + upto > begin);
+            const int from = later != 0u ? __ffs(int(later)) - 1 : 32;           // the first that reaches into the piece
+            at += __shfl_sync(0xffffffffu, from > 0 ? upto : 0L, from > 0 ? from - 1 : 0);
+#pragma unroll 1
+            for (int i = from; i < 32 && b0 + i < p.B && at < end && ok; ++i) {
+                const long hc = __shfl_sync(0xffffffffu, mine, i);
                 if (hc == 0) continue;
-                const int mts = row_tiles<C>(s, group);
-                long hd = quotient(in, hc);
-                in -= hd * hc;
-                for (; hd < heads && left > 0 && ok; ++hd) {
-                    for (int m = 0; m < mts && left > 0 && ok; ++m) {
-                        const long uc = unit_cost<C>(s, group, m);
-                        if (in >= uc) { in -= uc; continue; }
-                        // the unit's ends stand before its tiles; a tile is whose piece its beginning is in
-                        const int ut = int(unit_tiles<C>(s, group, m)), w = tile_cost<C>(s, group, m);
-                        auto tile_at = [&](long x) { return int(min(long(ut), max(0L, (x - C::kEnds + w - 1) / w))); };
-                        const long take = min(left, uc - in);
-                        Rec x{};
-                        x.t0 = tile_at(in);
-                        x.t1 = tile_at(in + take);
-                        if (x.t1 > x.t0) {
-                            x.l = int(hd) / p.HK; x.b = b; x.hk = int(hd) - x.l * p.HK; x.base = s.base; x.n = s.n; x.len = s.len;
-                            x.row0 = m * C::MT;
-                            x.rows = min(C::MT, s.n * group - x.row0);
-                            x.ct = s.ct;
-                            x.nodes = nodes_seen<C::MT>(s.n, group, m);
-                            x.slot = x.t0 == 0 && x.t1 == ut ? -1 : x.t0 == 0 ? 1 : 0;
-                            if (x.slot == 1) {
-                                // the unit ends in a later CTA's piece: where its last tile begins
-                                const long last = begin + (count - left) - in + C::kEnds + long(ut - 1) * w, wide = extra * (per + 1);
-                                const int owner = int(last < wide ? quotient(last, per + 1) : extra + quotient(last - wide, per));
-                                join = Join{owner - cta + 1, x.l, x.hk, x.base, x.row0, x.rows, 0, 0};
-                            }
-                            put(x);
-                        }
-                        left -= take;
-                        in = 0;
-                    }
+                Seq q;
+                q.base = __shfl_sync(0xffffffffu, s.base, i);
+                q.n = __shfl_sync(0xffffffffu, s.n, i);
+                q.len = __shfl_sync(0xffffffffu, s.len, i);
+                q.ct = __shfl_sync(0xffffffffu, s.ct, i);
+                const int mts = row_tiles<C>(q, group);
+                int hd = 0;
+                if (at < begin) {
+                    hd = int(quotient(begin - at, hc));
+                    at += hd * hc;
                 }
+#pragma unroll 1
+                for (; hd < heads && at < end && ok; ++hd)
+#pragma unroll 1
+                    for (int m = 0; m < mts && at < end && ok; ++m) {
+                        const int ut = int(unit_tiles<C>(q, group, m)), w = tile_cost<C>(q, group, m);
+                        const long tiles_at = at + C::kEnds;                     // the unit's ends stand before its tiles
+                        at = tiles_at + long(ut) * w;
+                        if (at <= begin) continue;
+                        // a tile is whose piece its beginning is in
+                        auto tile_from = [&](long x) { return x <= tiles_at ? 0 : int(min(long(ut), (x - tiles_at + w - 1) >> (w - 1))); };
+                        Rec x{};
+                        x.t0 = tile_from(begin);
+                        x.t1 = tile_from(end);
+                        if (x.t1 <= x.t0) continue;
+                        x.l = hd / p.HK; x.b = b0 + i; x.hk = hd - x.l * p.HK; x.base = q.base; x.n = q.n; x.len = q.len;
+                        x.row0 = m * C::MT;
+                        x.rows = min(C::MT, q.n * group - x.row0);
+                        x.ct = q.ct;
+                        x.nodes = nodes_seen<C::MT>(q.n, group, m);
+                        x.slot = x.t0 == 0 && x.t1 == ut ? -1 : x.t0 == 0 ? 1 : 0;
+                        put(x);
+                        if (x.slot == 1) {
+                            // the unit ends in a later CTA's piece: where its last tile begins
+                            const long last = tiles_at + long(ut - 1) * w, wide = extra * (per + 1);
+                            const int owner = int(last < wide ? quotient(last, per + 1) : extra + quotient(last - wide, per));
+                            join = Join{owner - cta + 1, x.l, x.hk, x.base, x.row0, x.rows, 0, 0};
+                        }
+                    }
+                if (hd < heads) break;
             }
         }
         if (ok) put(Rec{});
@@ -388,6 +383,24 @@ template <class C> struct Cta {
         }
     }
 };
+
+// Barrier of `THREADS` threads' worth of warps, and whether all of them are well: a warp whose wait gave up comes to the next one
+// once more, and all leave there together.  (An mbarrier that all arrive and wait on did the same in 250 ns; a segment has
+// three to six.)
+template <int THREADS> __device__ __forceinline__ bool all_well(bool ok)
+{
+    uint32_t r;
+    __syncwarp();
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 q, %1, 0;\n\t"
+        "bar.red.and.pred p, 1, %2, q;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(r)
+        : "r"(uint32_t(ok)), "n"(THREADS)
+        : "memory");
+    return r != 0u;
+}
 
 // the four maps of a call (a box of the cache is a page, or a tile's rows of one); 0 or an error
 template <int D> inline int encode_maps(const AttnParams &p, int box_rows, Maps &maps)

@@ -33,11 +33,11 @@ template <int DH> struct Few {
     static constexpr int KS = D == 64 ? 6 : 3, VS = KS;
     static constexpr int OffRing = 0;
     static constexpr int OffQ = (KS + VS) * TILE;            // queries; at a unit's end the warps' sums, float [warp][row][64]
-    static constexpr int OffPar = OffQ + kConsumers * kRows * 64 * 4;        // scratch of the scan, then int16 parent[kRows]
+    static constexpr int OffPar = OffQ + kConsumers * kRows * 64 * 4;        // int16 parent[kRows]
     static constexpr int OffMl = OffPar + 128;               // float2 [warp][row]
     static constexpr int OffRec = OffMl + kConsumers * kRows * 8;
     static constexpr int OffBars = OffRec + 64 * kRecords;
-    static constexpr int kKFull = 0, kKEmpty = KS, kVFull = 2 * KS, kVEmpty = kVFull + VS, kVRaw = 0, kSync = kVEmpty + VS, kRecFull = kSync + 1,
+    static constexpr int kKFull = 0, kKEmpty = KS, kVFull = 2 * KS, kVEmpty = kVFull + VS, kVRaw = 0, kRecFull = kVEmpty + VS,
                          kRecEmpty = kRecFull + kRecords, kBars = kRecEmpty + kRecords;
     static constexpr int OffMisc = OffBars + 8 * kBars;
     static constexpr int OffFlags = OffMisc + 64;
@@ -88,10 +88,9 @@ attend_few_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, in
     const int warp = x.warp, lane = x.lane, group = x.group, cta = blockIdx.x;
     if (warp == 0) {
         x.init(kConsumers + 2, kConsumers);
-        if (lane == 0) mbar_init(x.bar(C::kSync), kConsumers);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    x.find_piece();
+    x.begin();
 
     if (warp == kConsumers) x.template load<0>(maps, box_rows);
     else if (warp == kConsumers + 2) x.template load<1>(maps, box_rows);
@@ -104,16 +103,13 @@ attend_few_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, in
         int16_t *par = reinterpret_cast<int16_t *>(smem + C::OffPar);
         float2 *ml = reinterpret_cast<float2 *>(smem + C::OffMl);
         float *stage = reinterpret_cast<float *>(smem + C::OffQ);
-        uint32_t syncs = 0, keys = 0;                        // keys: tiles of the segments before
-        auto sync = [&]() -> bool {
-            __syncwarp();
-            if (lane == 0) mbar_arrive(x.bar(C::kSync));
-            return wait_fast(x.bar(C::kSync), syncs++ & 1, x.abort_flag);
-        };
+        uint32_t keys = 0;                                   // tiles of the segments before
+        auto sync = [&]() { return x.ok = all_well<kConsumers * 32>(x.ok); };
         Rec r;
-        for (uint32_t seg = 0; x.ok && x.record(seg, r); ++seg) {
+        for (uint32_t seg = 0;; ++seg) {
+            const bool more = x.record(seg, r);
+            if (!sync() || !more) break;                     // everyone is through with the last segment
             const bool tree = p.parent != nullptr && r.t1 > r.ct;
-            if (!(x.ok = sync())) break;                     // everyone is through with the last segment
             if (threadIdx.x == 0) x.topo_bad[(seg & 1) ^ 1] = 0;
             for (int i = threadIdx.x; i < r.rows * (D / 8); i += kConsumers * 32) {
                 const int row = i / (D / 8), c = i % (D / 8), at = r.row0 + row, node = at / group, g = at - node * group;
@@ -132,7 +128,7 @@ attend_few_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, in
                 }
             }
             copy16_wait();
-            if (!(x.ok = sync())) break;
+            if (!sync()) break;
             // this lane's rows of the unit, and the draft nodes they attend (no more nodes than rows)
             const int row0 = lane >> 2;
             uint32_t seen[2] = {0u, 0u};
@@ -259,7 +255,6 @@ attend_few_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, in
                 __syncwarp();
                 if (lane == 0) mbar_arrive(x.bar(C::kVEmpty + vs));
             }
-            if (!x.ok) break;
 
             // ---- end of the segment: the warps' sums are joined in the order of their keys
             if (__any_sync(0xffffffffu, mend) && lane == 0) x.value_bad[seg % kFlagRing] = int(seg) + 1;
@@ -269,7 +264,7 @@ attend_few_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, in
                 l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
                 if ((lane & 3) == 0) ml[warp * kRows + row0 + 8 * h] = make_float2(m[h], l[h]);
             }
-            if (!(x.ok = sync())) break;                     // (the queries have been used by all)
+            if (!sync()) break;                              // (the queries have been used by all)
             const bool skip = (x.topo_bad[seg & 1] != 0 && tree) || x.page_bad[seg % kFlagRing] == int(seg) + 1;
             const bool put_back = x.value_bad[seg % kFlagRing] == int(seg) + 1;
             float *sums = r.slot >= 0 ? slot_sums(plan, cta, r.slot) : nullptr;
@@ -280,14 +275,14 @@ attend_few_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, in
             if (sums != nullptr && threadIdx.x == 0) reinterpret_cast<int *>(sums + size_t(plan.rows_cap) * (D + 2))[0] = skip;
 #pragma unroll
             for (int turn = 0; turn < OC / 64; ++turn) {
-                if (turn > 0 && !(x.ok = sync())) break;
+                if (turn > 0 && !sync()) break;
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
                         *reinterpret_cast<float2 *>(stage + stage_offset(warp, row0 + 8 * h, 8 * j + (lane & 3) * 2)) =
                             make_float2(o[8 * turn + j][2 * h], o[8 * turn + j][2 * h + 1]);
-                if (!(x.ok = sync())) break;
+                if (!sync()) break;
                 // four columns of a row a thread, of the 64 that each group of warps has put there
 #pragma unroll 1
                 for (int u = threadIdx.x; u < r.rows * (C::CH * 16) && !skip; u += kConsumers * 32) {
@@ -316,8 +311,8 @@ attend_few_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, in
             }
             if (!x.ok) break;
             // (what other threads wrote is read back)
-            if (put_back && !skip && !(x.ok = sync())) break;
-            if (x.ok && put_back && !skip)
+            if (put_back && !skip && !sync()) break;
+            if (put_back && !skip)
                 for (int u = threadIdx.x; u < r.rows * D; u += kConsumers * 32) {
                     // (column u % D of a row; what other threads have written of it is behind the last sync)
                     const int row = u / D, col = u % D;
