@@ -20,26 +20,32 @@ namespace {
 
 constexpr float kSlack = 8.f;            // binary digits a maximum may grow by before O is scaled
 
-// D <= 128: two softmax groups of 128 rows, each with an O and a buffer for S of its own.  A unit of at most 128 rows has its
-// even key tiles in one and the odd ones in the other, joined at the end; a larger one has a row tile in each, over the same
-// keys.  D = 256: O alone takes half of TMEM, and there is one group, over tiles of half as many keys in three buffers.
-// P takes the first half of the columns of its S.  One warp asks for scores, another for the products with V, so that neither's waits
-// hold the other up (a loop over one item takes 1200 cycles beside its 12 products where one warp does both).
-template <int DH> struct Cfg {
+// D <= 128: two softmax groups of 128 rows, each with an O of its own.  A unit of at most 128 rows has its even key tiles in one
+// and the odd ones in the other, joined at the end; a larger one has a row tile in each, over the same keys.  D = 256: O alone
+// takes half of TMEM, and there is one group.  P takes the first half of the columns of its S.  One warp asks for scores, another
+// for the products with V, so that neither's waits hold the other up (a loop over one item takes 1200 cycles beside its 12
+// products where one warp does both).
+// MANY: units of more than 128 rows.  Products and softmax bound these: tiles of 64 keys leave room for a second buffer of S in
+// each group, formed while it works on the first (1024 prompt tokens behind 1500 and 4096: 166 us, tiles of 128 180).  Up to
+// 128 rows it is the keys' bytes: tiles of 128, and the second row tile's queries make room for one more of each ring (32 trees
+// of 64 rows 115 us, tiles of 64 125).
+template <int DH, bool MANY> struct Cfg {
     static constexpr int D = DH;
-    static constexpr int N = D == 256 ? 64 : 128;
     static constexpr int LANES = D == 256 ? 1 : 2;
-    static constexpr int BUFS = LANES == 2 ? 2 : 3;
-    static constexpr int MT = 128 * LANES;
-    static constexpr int kEnds = D == 256 ? 5 : 3;           // a unit's beginning and end in tiles: 8000 to 17000 cycles, a tile 2500 to 3500
+    static constexpr int N = MANY || D == 256 ? 64 : 128;
+    static constexpr int BUFS = LANES == 1 ? 3 : MANY ? 4 : 2;
+    static constexpr int MT = MANY && LANES == 2 ? 256 : 128;
+    static constexpr int kEnds = N == 128 ? 5 : D == 256 ? 8 : 10;          // a unit's beginning and end in tiles: some 15000 cycles
     static constexpr bool kMend = true;
     static constexpr int SOFT = 4 * LANES;                   // softmax warps; then keys, scores, products with V, mending of V, schedule, values
     static constexpr int THREADS = (SOFT + 6) * 32;
-    static constexpr int Q_BYTES = 128 * D * 2;
+    static constexpr int Q_BYTES = 128 * D * 2;              // queries of a row tile; at a unit's end sums on their way, 4096 bytes a warp
+    static constexpr int Q_ALL = Q_BYTES * (MT / 128) > 4096 * SOFT ? Q_BYTES * (MT / 128) : 4096 * SOFT;
     static constexpr int TILE = N * D * 2;                   // keys or values of a tile
-    static constexpr int KS = D == 64 ? 5 : 2, VS = D == 64 ? 5 : 3;       // tiles of keys and of values in flight or in use
+    static constexpr int FIT = (228 * 1024 - Q_ALL) / TILE - (D == 64 ? 1 : 0);                  // tiles in flight or in use
+    static constexpr int KS = FIT / 2, VS = FIT - KS;
     static constexpr int OffQ = 0;
-    static constexpr int OffRing = LANES * Q_BYTES;
+    static constexpr int OffRing = Q_ALL;
     static constexpr int OffPar = OffRing + (KS + VS) * TILE;    // int16 parent[kAttnMaxTree]
     static constexpr int OffRec = OffPar + 2 * kAttnMaxTree;
     static constexpr int OffBars = OffRec + 64 * kRecords;
@@ -50,7 +56,9 @@ template <int DH> struct Cfg {
     static constexpr int OffFlags = OffMisc + 64;            // segment numbers: bad page [8], values that are not finite [8]
     static constexpr int Bytes = OffFlags + 8 * kFlagRing;
 };
-static_assert(Cfg<128>::Bytes <= 232448 && Cfg<256>::Bytes <= 232448 && Cfg<64>::Bytes <= 232448, "shared memory of a CTA");
+template <class C> constexpr bool fits() { return C::Bytes <= 232448 && C::KS >= 2 && C::VS >= 2; }
+static_assert(fits<Cfg<64, false>>() && fits<Cfg<64, true>>() && fits<Cfg<128, false>>() && fits<Cfg<128, true>>() && fits<Cfg<256, true>>(),
+              "shared memory of a CTA");
 
 constexpr int kTmemCols = 512, kOCol = 256;                  // S (P) buffers from 0, N columns each, O from column 256
 
@@ -147,12 +155,12 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
-template <int D>
-__global__ void __launch_bounds__(Cfg<D>::THREADS, 1)
+template <int D, bool MANY>
+__global__ void __launch_bounds__(Cfg<D, MANY>::THREADS, 1)
 attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_t box_rows)
 {
     after_previous_kernel();
-    using C = Cfg<D>;
+    using C = Cfg<D, MANY>;
     constexpr int N = C::N, LANES = C::LANES, BUFS = C::BUFS, SOFT = C::SOFT, KS = C::KS, VS = C::VS;
     extern __shared__ __align__(1024) uint8_t smem[];
     Cta<C> x(p, plan, smem);
@@ -185,7 +193,7 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
     auto valid_of = [&](const Rec &r, int t) { return x.valid_of(r, t); };
     // Buffer of item i of a segment.  Every use of a buffer is one phase of its three barriers (scores there, weights there,
     // weights used); a role keeps the parity of the next one, a bit a buffer.
-    auto buffer = [](int i) { return LANES == 2 ? i & 1 : i % 3; };
+    auto buffer = [](int i) { return LANES == 2 ? i & (BUFS - 1) : i % 3; };
     Rec r;
 
     if (warp == SOFT) {
@@ -196,7 +204,7 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
         const uint32_t id_s = make_idesc_bf16(N);
         uint32_t loads = 0, phase = 0;                       // tiles of the segments before; next parities
         for (uint32_t seg = 0; ok && record(seg, r); ++seg) {
-            const bool two = LANES == 2 && r.rows > 128;     // two row tiles over the same keys
+            const bool two = C::MT == 256 && r.rows > 128;     // two row tiles over the same keys
             const int tiles = r.t1 - r.t0, items = tiles << (two ? 1 : 0);
             if (!(ok = wait_fast(bar(C::kQFull), seg & 1, abort_flag))) break;
             tc_fence_after();
@@ -224,7 +232,7 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
         const uint32_t id_o = make_idesc_bf16(D) | (1u << 16);   // (B is MN-major)
         uint32_t loads = 0, phase = 0;
         for (uint32_t seg = 0; ok && record(seg, r); ++seg) {
-            const bool two = LANES == 2 && r.rows > 128;
+            const bool two = C::MT == 256 && r.rows > 128;
             const int tiles = r.t1 - r.t0, items = tiles << (two ? 1 : 0);
 #pragma unroll 1
             for (int i = 0; i < items; ++i) {
@@ -307,7 +315,7 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
         for (uint32_t seg = 0;; ++seg) {
             const bool more = record(seg, r);
             if (!sync() || !more) break;                     // everyone is through with the last segment: its queries, its parents
-            const bool two = LANES == 2 && r.rows > 128;
+            const bool two = C::MT == 256 && r.rows > 128;
             const int tiles = r.t1 - r.t0;
             const int all = tiles << (two ? 1 : 0);          // items of both groups
             if (threadIdx.x == 0) topo_bad[(seg & 1) ^ 1] = 0;
@@ -497,7 +505,7 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
                 if (sums == nullptr) { f0 *= inv; f1 *= inv; }
                 // Through shared memory (this group's queries have been used), so that a row is written in whole lines: straight
                 // from the lanes, a row each, a store touched 32 lines, and 128 rows took 9000 cycles.
-                uint8_t *stage = smem + C::OffQ + (LANES == 2 ? wg : 0) * C::Q_BYTES + quad * 4096;
+                uint8_t *stage = smem + C::OffQ + (two ? wg * C::Q_BYTES : wg * 16384) + quad * 4096;
                 const uint64_t out_at = reinterpret_cast<uint64_t>(out);
                 const int rows_here = min(32, r.rows - (row - lane));
 #pragma unroll 1
@@ -664,40 +672,58 @@ join_kernel(AttnParams p, Plan plan, int32_t blocks)
 inline int unit_rows(int max_nodes, int group, int d)
 {
     const long rows = long(max_nodes) * group;
-    const int few = attend_few_rows(rows), mt = few > 0 ? few : d == 256 ? Cfg<256>::MT : Cfg<128>::MT;
+    const int few = attend_few_rows(rows), mt = few > 0 ? few : d == 256 ? Cfg<256, true>::MT : Cfg<128, true>::MT;
     return rows < mt ? int(rows) : mt;
 }
 
 std::atomic<bool> g_opted_in[64];                            // per device: shared memory of every instantiation
 
-template <int D> int launch_width(const AttnParams &p, cudaStream_t st)
+int opt_in()
 {
-    using C = Cfg<D>;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return int(cudaErrorInvalidDevice);
+    if (g_opted_in[dev].load(std::memory_order_acquire)) return 0;
+    cudaError_t e = cudaSuccess;
+    auto one = [&](const void *k, int bytes) {
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    };
+    one(reinterpret_cast<const void *>(attend_kernel<64, false>), Cfg<64, false>::Bytes);
+    one(reinterpret_cast<const void *>(attend_kernel<64, true>), Cfg<64, true>::Bytes);
+    one(reinterpret_cast<const void *>(attend_kernel<128, false>), Cfg<128, false>::Bytes);
+    one(reinterpret_cast<const void *>(attend_kernel<128, true>), Cfg<128, true>::Bytes);
+    one(reinterpret_cast<const void *>(attend_kernel<256, true>), Cfg<256, true>::Bytes);
+    if (e == cudaSuccess) g_opted_in[dev].store(true, std::memory_order_release);
+    return int(e);
+}
+
+template <int D> int launch_width(const AttnParams &p, cudaStream_t st)
+{
     const int sms = sm_count_of_current_device();
     if (sms <= 0) return int(cudaErrorInvalidDevice);
-    if (!g_opted_in[dev].load(std::memory_order_acquire)) {
-        cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void *>(attend_kernel<64>), cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<64>::Bytes);
-        if (e == cudaSuccess)
-            e = cudaFuncSetAttribute(reinterpret_cast<const void *>(attend_kernel<128>), cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<128>::Bytes);
-        if (e == cudaSuccess)
-            e = cudaFuncSetAttribute(reinterpret_cast<const void *>(attend_kernel<256>), cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<256>::Bytes);
-        if (e != cudaSuccess) return int(e);
-        g_opted_in[dev].store(true, std::memory_order_release);
-    }
-    const int page = 1 << p.page_shift, box_rows = page < C::N ? page : C::N, grid = sms < kMaxCtas ? sms : kMaxCtas;
+    const int rows_cap = unit_rows(p.max_nodes, p.H / p.HK, D), page = 1 << p.page_shift, grid = sms < kMaxCtas ? sms : kMaxCtas;
+    const Plan plan = make_plan(p, rows_cap, D);
     Maps maps;
-    const int rc = encode_maps<D>(p, box_rows, maps);
-    if (rc != 0) return rc;
-    const Plan plan = make_plan(p, unit_rows(p.max_nodes, p.H / p.HK, D), D);
-    if (attend_few_rows(long(p.max_nodes) * (p.H / p.HK)) > 0) {
-        const int r = launch_attend_few(p, D, maps, plan, box_rows, grid, st);
-        if (r != 0) return r;
-    } else launch(attend_kernel<D>, grid, C::THREADS, C::Bytes, st, maps, p, plan, int32_t(box_rows));
-    const int e = int(cudaGetLastError());
+    // `keys` a tile: a box of the cache is a page, or a tile's part of one
+    auto go = [&](int keys, auto launch_it) {
+        const int box_rows = page < keys ? page : keys, rc = encode_maps<D>(p, box_rows, maps);
+        return rc != 0 ? rc : launch_it(box_rows);
+    };
+    int e = opt_in();
     if (e != 0) return e;
-    const int blocks = (plan.rows_cap + kJoinWarps - 1) / kJoinWarps;
+    if (attend_few_rows(long(p.max_nodes) * (p.H / p.HK)) > 0)
+        e = go(D == 256 ? 64 : 128, [&](int box) { return launch_attend_few(p, D, maps, plan, box, grid, st); });
+    else if (D == 256 || rows_cap > 128)
+        e = go(64, [&](int box) {
+            launch(attend_kernel<D, true>, grid, Cfg<D, true>::THREADS, Cfg<D, true>::Bytes, st, maps, p, plan, int32_t(box));
+            return int(cudaGetLastError());
+        });
+    else if constexpr (D != 256)
+        e = go(128, [&](int box) {
+            launch(attend_kernel<D, false>, grid, Cfg<D, false>::THREADS, Cfg<D, false>::Bytes, st, maps, p, plan, int32_t(box));
+            return int(cudaGetLastError());
+        });
+    if (e != 0) return e;
+    const int blocks = (rows_cap + kJoinWarps - 1) / kJoinWarps;
     launch(join_kernel<D>, unsigned(grid * blocks), kJoinWarps * 32, 0, st, p, plan, int32_t(blocks));
     return int(cudaGetLastError());
 }

@@ -123,7 +123,7 @@ template <class C> __device__ __forceinline__ long unit_tiles(const Seq &s, int 
 // short sequences took up to twice as long as the others.
 template <class C> __device__ __forceinline__ int tile_cost(const Seq &s, int group, int m)
 {
-    return C::LANES == 2 && s.n * group - m * C::MT > 128 ? 2 : 1;
+    return C::MT == 256 && s.n * group - m * C::MT > 128 ? 2 : 1;
 }
 template <class C> __device__ __forceinline__ long unit_cost(const Seq &s, int group, int m)
 {
@@ -152,8 +152,8 @@ struct Maps {
     CUtensorMap k, v, k_draft, v_draft;
 };
 
-// A CTA's view of the work.  C: N keys a tile, D columns, MT rows of a unit, THREADS, kEnds, LANES, KS and VS slots of TILE bytes
-// at OffRing (keys, then values), barriers from OffBars, scratch of 8 * THREADS / 32 bytes at OffPar.
+// A CTA's view of the work.  C: N keys a tile, D columns, MT rows of a unit, kEnds, KS and VS slots of TILE bytes
+// at OffRing (keys, then values), barriers from OffBars.
 // (A barrier has two parities: whoever waits on one waits for all its phases in turn.  So keys and values have rings of their
 // own, and where C::kMend, values that are looked over before they are used land on barriers of their own.)
 template <class C> struct Cta {
@@ -285,6 +285,9 @@ template <class C> struct Cta {
         Join join{0, 0, 0, 0, 0, 0, 0, 0};
         uint32_t seg = 0;
         auto put = [&](const Rec &x) {
+            // the unit's queries are asked into L2 while the segments before it are worked on
+            for (int node = x.row0 / group + lane; node * group < x.row0 + x.rows; node += 32)
+                prefetch_l2(p.q + ((size_t(x.l) * p.T + x.base + node) * p.H + x.hk * group) * D, uint32_t(group) * D * 2);
             ok = seg < kRecords || wait_fast(bar(C::kRecEmpty + (seg % kRecords)), ((seg / kRecords) & 1) ^ 1, abort_flag);
             if (!ok) return;
             if (lane == 0) {
@@ -314,7 +317,7 @@ template <class C> struct Cta {
         for (int i = 16; i > 0; i /= 2) total += __shfl_xor_sync(0xffffffffu, total, i);
         total *= heads;
         // (a piece is at least one tile long, so that every CTA between a unit's first and last has some of it)
-        const int pieces = int(min(long(grid), max(1L, total / (plan.rows_cap > 128 ? 2 : 1))));
+        const int pieces = int(min(long(grid), max(1L, total / (C::MT == 256 ? 2 : 1))));
         const long per = quotient(total, pieces), extra = total - per * pieces;
         const long begin = cta * per + min(long(cta), extra), end = cta < pieces ? begin + per + (cta < extra ? 1 : 0) : begin;
         long at = 0;                                         // place in the list of the sequence looked at
