@@ -382,7 +382,7 @@ int speca_verify_tree_noalloc(const speca_dims *dims, const float *S0,
 typedef struct speca_attn_dims {
     int32_t n_layers;    /* L >= 1                                                    */
     int32_t batch;       /* B >= 1                                                    */
-    int32_t heads;       /* query heads, a multiple of kv_heads                       */
+    int32_t heads;       /* query heads, a multiple of kv_heads, at most 4096        */
     int32_t kv_heads;    /* key and value heads >= 1                                  */
     int32_t d_head;      /* 64, 128 or 256                                            */
     float   scale;       /* softmax(scale * q k^T), > 0; usually d_head ^ -1/2        */

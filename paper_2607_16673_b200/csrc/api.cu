@@ -42,8 +42,8 @@ int check_attn_dims(const speca_attn_dims *d)
     if (d->heads % d->kv_heads != 0) return SPECA_ERR_UNSUPPORTED;
     if (d->d_head != 64 && d->d_head != 128 && d->d_head != 256) return SPECA_ERR_UNSUPPORTED;
     if (d->page_size < 16 || d->page_size > 256 || (d->page_size & (d->page_size - 1)) != 0) return SPECA_ERR_UNSUPPORTED;
-    // rows of the pool are TMA coordinates, head rows of a token and rows of a sequence 32-bit numbers
-    if (d->heads > 65536 || d->n_layers > 65536 || d->batch > (1 << 24)) return SPECA_ERR_RANGE;
+    // rows of the pool are TMA coordinates; rows of a sequence, and what a prompt appends in 16-byte pieces, 32-bit numbers
+    if (d->heads > 4096 || d->n_layers > 65536 || d->batch > (1 << 24)) return SPECA_ERR_RANGE;
     const double rows = double(d->n_layers) * d->n_pages * d->kv_heads * d->page_size;
     if (rows > 2147483647.0 || 1LL * d->max_pages * d->page_size > 0x7fffffffLL) return SPECA_ERR_RANGE;
     return SPECA_OK;

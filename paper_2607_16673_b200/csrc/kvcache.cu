@@ -9,13 +9,36 @@ namespace {
 // Norm and rotation.  A warp takes a share of one token's head rows over all layers.  D / 8 lanes have a row, and a lane has both
 // elements of four pairs (lanes beyond the rotated part: eight plain elements), so no element travels between lanes but for
 // the sum of squares, and its four angles are the same for every row of the token: they are formed once.  Weights, cosines and
-// sines of a layer's queries (or keys) are multiplied out beforehand, which leaves eight products, eight fused multiply-adds
-// and the scale by the norm a row.  The rows of the next step are asked for before this one's are worked on.
+// sines of a layer's queries (or keys) are multiplied out beforehand, which leaves a product, a fused multiply-add and the scale
+// by the norm for each pair of elements.  The rows of the next step are asked for before this one's are worked on.
 // ---------------------------------------------------------------------------------------------------------------
-constexpr int kNormWarps = 4, kNormRows = 4;                // rows a lane has in flight
+constexpr int kNormWarps = 4, kNormRows = 4;                // rows a lane has in flight (2: 245 us for 5632 tokens in 12 layers, 4: 215, 8: 311)
+constexpr int kNormBlocks = 5;                              // an SM: 96 registers (left to itself the compiler takes more, 241 us)
 
-__device__ __forceinline__ uint32_t pack2(float lo, float hi)
+// two fp32 values in a pair of registers, one instruction for both
+__device__ __forceinline__ uint64_t pair2(float lo, float hi)
 {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpair2(uint64_t x, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack2(uint64_t x)
+{
+    float lo, hi;
+    unpair2(x, lo, hi);
     const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&h);
 }
@@ -29,7 +52,7 @@ __device__ __forceinline__ int sequence_of(const int32_t *node_offsets, int B, i
 }
 
 template <int D, bool INTER>
-__global__ void __launch_bounds__(kNormWarps * 32)
+__global__ void __launch_bounds__(kNormWarps * 32, kNormBlocks)
 norm_rope_kernel(AttnParams p, NormParams np, int32_t parts)
 {
     after_previous_kernel();
@@ -105,8 +128,8 @@ norm_rope_kernel(AttnParams p, NormParams np, int32_t parts)
         }
     }
 
-    // first <- first * k0 - second * k1, second <- first * k2 + second * k3 of pair i, before the norm's scale
-    float k0[4], k1[4], k2[4], k3[4];
+    // element <- element * own + mate * other, before the norm's scale; in pairs as below
+    uint64_t own[4], other[4];
     int made = -1;                                          // 2 * layer + (keys) that they are for
     while (it < end) {
         const bool is_q = s < steps_q;
@@ -126,8 +149,17 @@ norm_rope_kernel(AttnParams p, NormParams np, int32_t parts)
             const float x[8] = {wa.x, wa.y, wa.z, wa.w, wb.x, wb.y, wb.z, wb.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float f = INTER ? x[2 * i] : x[i], g = INTER ? x[2 * i + 1] : x[4 + i];
-                k0[i] = f * cs[i]; k1[i] = g * sn[i]; k2[i] = f * sn[i]; k3[i] = g * cs[i];
+                // elements 2 i and 2 i + 1; of the half layout those of the second half (i >= 2) turn the other way
+                const int e = 2 * i;
+                if (INTER) {
+                    own[i] = pair2(x[e] * cs[i], x[e + 1] * cs[i]);
+                    other[i] = pair2(-x[e + 1] * sn[i], x[e] * sn[i]);
+                } else {
+                    const int f = e & 3, m = e ^ 4;
+                    const float s0 = i < 2 ? -sn[f] : sn[f], s1 = i < 2 ? -sn[f + 1] : sn[f + 1];
+                    own[i] = pair2(x[e] * cs[f], x[e + 1] * cs[f + 1]);
+                    other[i] = pair2(x[m] * s0, x[m + 1] * s1);
+                }
             }
         }
         const int h0 = (is_q ? s : s - steps_q) * HPW + sub, heads = is_q ? p.H : p.HK;
@@ -135,33 +167,43 @@ norm_rope_kernel(AttnParams p, NormParams np, int32_t parts)
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (u < m) {
+                // pairs of elements: (0, 1) and (2, 3) of each half, so that one instruction works on two
                 const uint32_t raw[4] = {a[u].x, a[u].y, b[u].x, b[u].y};
-                float x[8], y[8];
+                uint64_t x[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    x[2 * i] = __uint_as_float(raw[i] << 16);
-                    x[2 * i + 1] = __uint_as_float(raw[i] & 0xffff0000u);
-                }
+                for (int i = 0; i < 4; ++i) x[i] = pair2(__uint_as_float(raw[i] << 16), __uint_as_float(raw[i] & 0xffff0000u));
                 float rs = 1.f;
                 if (w != nullptr) {
-                    float sum = 0.f;
+                    uint64_t sq = mul2(x[0], x[0]);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], sum);
+                    for (int i = 1; i < 4; ++i) sq = fma2(x[i], x[i], sq);
+                    float lo, hi;
+                    unpair2(sq, lo, hi);
+                    float sum = lo + hi;
 #pragma unroll
                     for (int j = LPH / 2; j > 0; j /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, j);
                     rs = rsqrtf(sum * (1.f / D) + np.eps);
                 }
+                const uint64_t rs2 = pair2(rs, rs);
+                uint64_t y[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int e = INTER ? 2 * i : i, f = INTER ? 2 * i + 1 : 4 + i;
-                    // (a plain element takes nothing from its neighbour, not even what is not finite)
-                    y[e] = turned ? fmaf(x[e], k0[i], -(x[f] * k1[i])) * rs : x[e] * k0[i] * rs;
-                    y[f] = turned ? fmaf(x[e], k2[i], x[f] * k3[i]) * rs : x[f] * k3[i] * rs;
+                    // what each element is rotated with: the same place of the other half, or its neighbour
+                    uint64_t mate = x[i ^ 2];
+                    if (INTER) {
+                        float lo, hi;
+                        unpair2(x[i], lo, hi);
+                        mate = pair2(hi, lo);
+                    }
+                    // (a plain element takes nothing from another, not even what is not finite)
+                    y[i] = mul2(x[i], own[i]);
+                    if (turned) y[i] = fma2(mate, other[i], y[i]);
+                    y[i] = mul2(y[i], rs2);
                 }
                 if (h0 + u * HPW < heads) {
                     __nv_bfloat16 *to = out + size_t(h0 + u * HPW) * D;
-                    *reinterpret_cast<uint2 *>(to + ea) = make_uint2(pack2(y[0], y[1]), pack2(y[2], y[3]));
-                    *reinterpret_cast<uint2 *>(to + eb) = make_uint2(pack2(y[4], y[5]), pack2(y[6], y[7]));
+                    *reinterpret_cast<uint2 *>(to + ea) = make_uint2(pack2(y[0]), pack2(y[1]));
+                    *reinterpret_cast<uint2 *>(to + eb) = make_uint2(pack2(y[2]), pack2(y[3]));
                 }
             }
         it = it2; s = s2; l = l2; m = m2;
@@ -174,60 +216,80 @@ norm_rope_kernel(AttnParams p, NormParams np, int32_t parts)
 // Commit of records to the cache: a CTA takes a share of what one sequence appends to one layer, 16 bytes a thread at a
 // time.  Rows of the records are [token][head], rows of the cache [page][head][row].
 // ---------------------------------------------------------------------------------------------------------------
-constexpr int kCommitThreads = 256;
+constexpr int kCommitThreads = 256, kCommitPieces = 4;       // 16-byte pieces of keys and of values a thread has in flight
 
 __global__ void __launch_bounds__(kCommitThreads)
 commit_kv_kernel(AttnParams p, int32_t vec, int32_t parts, int32_t *kv_len_out)
 {
     after_previous_kernel();
-    __shared__ int32_t node[16];
     const int part = blockIdx.x % parts, b = blockIdx.x / parts % p.B, l = blockIdx.x / parts / p.B, tid = threadIdx.x;
-    const int len = p.kv_len[b];
-    int base, n, A, fault = 0;
-    if (p.path_idx != nullptr) {
+    const bool path = p.path_idx != nullptr;
+    const int32_t *entry = p.path_idx + size_t(b) * p.max_depth, *table = p.page_table + size_t(b) * p.max_pages;
+    const int len = p.kv_len[b], base = p.node_offsets[b], stop = p.node_offsets[b + 1];
+    const int mine = path && tid < p.max_depth ? entry[tid] : 0, above = path && tid > 0 && tid < p.max_depth ? entry[tid - 1] : -1;
+    int n = stop - base, A = n, fault = 0;
+    if (path) {
         A = p.path_len[b];
-        base = p.node_offsets[b];
-        const int end = p.node_offsets[b + 1];
-        n = end - base;
         if (A < 0 || A > p.max_depth) fault = SPECA_STATUS_TOO_DEEP;
-        else if (A > 0 && (base < 0 || end < base || end > p.T)) fault = SPECA_STATUS_BAD_OFFSETS;
-        else if (tid < A) {
-            const int e = p.path_idx[size_t(b) * p.max_depth + tid];
-            node[tid] = e;
-            if (e < 0 || e >= n) fault = SPECA_STATUS_BAD_PATH;
-            else if (p.parent != nullptr &&
-                     p.parent[base + e] != (tid == 0 ? -1 : p.path_idx[size_t(b) * p.max_depth + tid - 1]))
-                fault = SPECA_STATUS_BAD_PATH;
-        }
+        else if (A > 0 && (base < 0 || stop < base || stop > p.T)) fault = SPECA_STATUS_BAD_OFFSETS;
     } else {
-        fault = sequence_nodes(p, b, base, n);
-        A = n;
+        int b0, n0;
+        fault = sequence_nodes(p, b, b0, n0);
     }
     const int page = 1 << p.page_shift;
-    const int32_t *table = p.page_table + size_t(b) * p.max_pages;
     if (!fault && (len < 0 || (A > 0 && 1LL * len + A > 1LL * p.max_pages * page))) fault = SPECA_STATUS_BAD_PAGE;
-    if (!fault && A > 0)
-        for (int i = (len >> p.page_shift) + tid; i <= (len + A - 1) >> p.page_shift; i += kCommitThreads)
-            if (table[i] < 0 || table[i] >= p.n_pages) fault = SPECA_STATUS_BAD_PAGE;
-    const bool lead = l == 0 && part == 0;
-    if (fault && lead) atomicOr(p.status, fault);
-    if (__syncthreads_or(fault)) {
-        if (lead && tid == 0 && kv_len_out != nullptr) kv_len_out[b] = len;
-        return;
-    }
-    if (lead && tid == 0 && kv_len_out != nullptr) kv_len_out[b] = len + A;
-    const int row = p.HK * vec, page_vec = page * vec;       // 16-byte pieces of a token's row, of a page of one head
-    const long total = long(A) * row;
+    const long total = fault ? 0 : long(A) * p.HK * vec;
+
+    // The first pieces are read while the path and the pages are still being checked, each by the thread that has it: what an
+    // index out of range would name is not.
+    const uint32_t row = uint32_t(p.HK) * vec;               // pieces of a token's row
     const uint4 *ks = reinterpret_cast<const uint4 *>(p.k), *vs = reinterpret_cast<const uint4 *>(p.v);
     uint4 *kc = reinterpret_cast<uint4 *>(p.k_cache), *vc = reinterpret_cast<uint4 *>(p.v_cache);
-    for (long i = long(part) * kCommitThreads + tid; i < total; i += long(parts) * kCommitThreads) {
-        const int a = int(i / row), r = int(i % row), h = r / vec, e = r % vec;
-        const int from = base + (p.path_idx != nullptr ? node[a] : a), at = len + a;
-        const size_t src = (size_t(l) * p.T + from) * row + r;
-        const size_t dst = ((size_t(l) * p.n_pages + table[at >> p.page_shift]) * p.HK + h) * page_vec + size_t(at & (page - 1)) * vec + e;
-        const uint4 x = ks[src], y = vs[src];
-        kc[dst] = x;
-        vc[dst] = y;
+    uint4 x[kCommitPieces], y[kCommitPieces];
+    size_t to[kCommitPieces];
+    auto fetch = [&](long first) {
+#pragma unroll
+        for (int j = 0; j < kCommitPieces; ++j) {
+            const long i = first + j * kCommitThreads;
+            to[j] = ~size_t(0);
+            if (i >= total) continue;
+            const int a = int(uint32_t(i) / row), at = len + a;                 // (less than 2^31 pieces: 8192 rows of 2^17 at most)
+            const uint32_t r = uint32_t(i) - a * row, h = r / vec, e = r - h * vec;
+            const int from = path ? entry[a] : a, id = table[at >> p.page_shift];
+            if (from < 0 || from >= n || id < 0 || id >= p.n_pages) continue;
+            const size_t src = (size_t(l) * p.T + base + from) * row + r;
+            to[j] = ((((size_t(l) * p.n_pages + id) * p.HK + h) << p.page_shift) + (at & (page - 1))) * vec + e;
+            x[j] = ks[src];
+            y[j] = vs[src];
+        }
+    };
+    auto put = [&]() {
+#pragma unroll
+        for (int j = 0; j < kCommitPieces; ++j)
+            if (to[j] != ~size_t(0)) {
+                kc[to[j]] = x[j];
+                vc[to[j]] = y[j];
+            }
+    };
+    const long first = long(part) * (kCommitThreads * kCommitPieces) + tid, stride = long(parts) * (kCommitThreads * kCommitPieces);
+    fetch(first);
+    if (!fault && A > 0) {
+        if (path && tid < A) {
+            if (mine < 0 || mine >= n) fault = SPECA_STATUS_BAD_PATH;
+            else if (p.parent != nullptr && p.parent[base + mine] != (tid == 0 ? -1 : above)) fault = SPECA_STATUS_BAD_PATH;
+        }
+        for (int i = (len >> p.page_shift) + tid; i <= (len + A - 1) >> p.page_shift; i += kCommitThreads)
+            if (table[i] < 0 || table[i] >= p.n_pages) fault = SPECA_STATUS_BAD_PAGE;
+    }
+    const bool lead = l == 0 && part == 0;
+    if (fault && lead) atomicOr(p.status, fault);
+    const bool skip = __syncthreads_or(fault);
+    if (lead && tid == 0 && kv_len_out != nullptr) kv_len_out[b] = skip ? len : len + A;
+    if (skip) return;
+    put();
+    for (long i = first + stride; i - tid < total; i += stride) {
+        fetch(i);
+        put();
     }
 }
 
@@ -315,8 +377,9 @@ int launch_norm_rope(const AttnParams &p, const NormParams &n, int d_head, cudaS
     const int hpw = 256 / d_head;
     const long steps = long(p.L) * ((p.H + hpw - 1) / hpw + (p.HK + hpw - 1) / hpw);
     // A token's rows stay with one warp, which then forms its angles once, as long as that makes enough warps to fill the
-    // machine; a few tokens are spread over as many warps as they have steps.
-    const long most = sms * 64;
+    // machine (8192 tokens of one layer 36.6 us, spread over three times as many warps 41.8); fewer tokens are spread over as
+    // many warps as they have steps.
+    const long most = sms * kNormWarps * kNormBlocks;
     long parts = p.T >= most ? 1 : (most + p.T - 1) / p.T;
     if (parts > steps) parts = steps;
     unsigned grid;
@@ -332,7 +395,7 @@ int launch_commit_kv(const AttnParams &p, int d_head, int32_t *kv_len_out, cudaS
 {
     const int vec = d_head / 8;
     const long most = long(p.path_idx != nullptr ? p.max_depth : p.max_nodes) * p.HK * vec;
-    long parts = (most + kCommitThreads * 4 - 1) / (kCommitThreads * 4);
+    long parts = (most + kCommitThreads * kCommitPieces - 1) / (kCommitThreads * kCommitPieces);
     const bool in_place = kv_len_out == p.kv_len;
     unsigned grid;
     const int rc = grid_of(parts * p.B * p.L, grid);
