@@ -598,74 +598,98 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// Units that several CTAs have a piece of: a warp a row, pieces in order, so that the result does not depend on which CTA
-// was ready first.
+// Units that several CTAs have a piece of: a warp some rows at a time, pieces in order, so that the result does not depend on
+// which CTA was ready first.  No more blocks than fit at once, and the sums of several rows and pieces asked for together: it is
+// round trips to L2 that this takes (a block for every eight rows of every CTA, six waves of them, took 20 us behind 141 of
+// prompt chunks).  FEW: units of few rows, which are few units if they are cut at all, and then into many pieces; larger ones
+// are cut into two or three.
 // ---------------------------------------------------------------------------------------------------------------
-constexpr int kJoinWarps = 8;
+constexpr int kJoinWarps = 8, kJoinBlocks = 4;               // blocks a CTA of the other kernel at most
 
-template <int D>
-__global__ void __launch_bounds__(kJoinWarps * 32)
+template <int D, bool FEW>
+__global__ void __launch_bounds__(kJoinWarps * 32, kJoinBlocks)
 join_kernel(AttnParams p, Plan plan, int32_t blocks)
 {
     after_previous_kernel();
+    constexpr int E = D / 32, PARTS = !FEW ? 2 : D == 256 ? 4 : 8, ROWS = FEW ? 1 : D == 256 ? 2 : 4;   // asked for together
     const int cta = blockIdx.x / blocks, lane = threadIdx.x & 31;
     const Join j = plan.join[cta];
-    const int row = (blockIdx.x % blocks) * kJoinWarps + (threadIdx.x >> 5);
-    if (j.parts <= 1 || row >= j.rows) return;
+    if (j.parts <= 1) return;
     const float c2 = p.scale * 1.4426950408889634f;
-    constexpr int E = D / 32, AT_ONCE = 8;
+    const int group = p.H / p.HK, step = blocks * kJoinWarps;
     auto part = [&](int i) { return slot_sums(plan, cta + i, i == 0 ? 1 : 0); };
-    float o[E], l = 0.f, m = -INFINITY;
-    int skip = 0;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = 0.f;
-    // eight parts at a time, their sums asked for together with their maxima (one round trip each)
 #pragma unroll 1
-    for (int i0 = 0; i0 < j.parts; i0 += AT_ONCE) {
-        float2 ml = make_float2(-INFINITY, 0.f);
-        float x[AT_ONCE][E];
-        if (lane < AT_ONCE && i0 + lane < j.parts) {
-            const float *tail = part(i0 + lane) + size_t(plan.rows_cap) * D;
-            ml = reinterpret_cast<const float2 *>(tail)[row];
-            skip |= reinterpret_cast<const int *>(tail + 2 * plan.rows_cap)[0];
+    for (int first = (blockIdx.x % blocks) * kJoinWarps + (threadIdx.x >> 5); first < j.rows; first += ROWS * step) {
+        float o[ROWS][E], l[ROWS], m[ROWS];
+        int skip = 0;
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            l[r] = 0.f;
+            m[r] = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[r][e] = 0.f;
         }
+#pragma unroll 1
+        for (int i0 = 0; i0 < j.parts; i0 += PARTS) {
+            float2 ml = make_float2(-INFINITY, 0.f);         // lane r * PARTS + i: of part i of row r
+            float x[ROWS][PARTS][E];
+            if (lane < ROWS * PARTS && i0 + lane % PARTS < j.parts) {
+                const float *tail = part(i0 + lane % PARTS) + size_t(plan.rows_cap) * D;
+                const int row = first + lane / PARTS * step;
+                if (row < j.rows) ml = reinterpret_cast<const float2 *>(tail)[row];
+                skip |= reinterpret_cast<const int *>(tail + 2 * plan.rows_cap)[0];
+            }
 #pragma unroll
-        for (int i = 0; i < AT_ONCE; ++i) {
+            for (int r = 0; r < ROWS; ++r)
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[i][e] = 0.f;
-            if (i0 + i < j.parts) {
-                const float *at = part(i0 + i) + size_t(row) * D + lane * E;
-                if constexpr (E == 2) *reinterpret_cast<float2 *>(x[i]) = *reinterpret_cast<const float2 *>(at);
-                else
+                for (int i = 0; i < PARTS; ++i) {
 #pragma unroll
-                    for (int e = 0; e < E; e += 4) *reinterpret_cast<float4 *>(x[i] + e) = *reinterpret_cast<const float4 *>(at + e);
+                    for (int e = 0; e < E; ++e) x[r][i][e] = 0.f;
+                    if (i0 + i < j.parts && first + r * step < j.rows) {
+                        const float *at = part(i0 + i) + size_t(first + r * step) * D + lane * E;
+                        if constexpr (E == 2) *reinterpret_cast<float2 *>(x[r][i]) = *reinterpret_cast<const float2 *>(at);
+                        else
+#pragma unroll
+                            for (int e = 0; e < E; e += 4) *reinterpret_cast<float4 *>(x[r][i] + e) = *reinterpret_cast<const float4 *>(at + e);
+                    }
+                }
+            float top = ml.x;
+#pragma unroll
+            for (int w = PARTS / 2; w > 0; w /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                const float now = fmaxf(m[r], __shfl_sync(0xffffffffu, top, r * PARTS));
+                // (what has nothing yet is zero in whatever scale)
+                const float old = m[r] == now || m[r] == -INFINITY ? 1.f : exp2_approx((m[r] - now) * c2);
+                m[r] = now;
+                l[r] *= old;
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[r][e] *= old;
+#pragma unroll
+                for (int i = 0; i < PARTS; ++i) {
+                    const float mi = __shfl_sync(0xffffffffu, ml.x, r * PARTS + i), li = __shfl_sync(0xffffffffu, ml.y, r * PARTS + i);
+                    const float f = mi == now || mi == -INFINITY ? 1.f : exp2_approx((mi - now) * c2);
+                    l[r] = fmaf(li, f, l[r]);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) o[r][e] = fmaf(x[r][i][e], f, o[r][e]);
+                }
             }
         }
-        float top = ml.x;
+        if (__any_sync(0xffffffffu, skip)) return;           // (the same for every row)
 #pragma unroll
-        for (int w = AT_ONCE / 2; w > 0; w /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
-        top = fmaxf(m, __shfl_sync(0xffffffffu, top, 0));
-        // (what has nothing yet is zero in whatever scale)
-        const float old = m == top || m == -INFINITY ? 1.f : exp2_approx((m - top) * c2);
-        const float mine = ml.x == top || ml.x == -INFINITY ? 1.f : exp2_approx((ml.x - top) * c2);
-        m = top;
-        l *= old;
+        for (int r = 0; r < ROWS; ++r) {
+            if (first + r * step >= j.rows) break;
+            const int at = j.row0 + first + r * step, node = at / group, g = at - node * group;
+            __nv_bfloat16 *to = p.o + ((size_t(j.l) * p.T + j.base + node) * p.H + j.hk * group + g) * D + lane * E;
+            const float inv = 1.f / l[r];
+            uint32_t y[E / 2];
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] *= old;
-#pragma unroll
-        for (int i = 0; i < AT_ONCE; ++i) {
-            const float f = __shfl_sync(0xffffffffu, mine, i);
-            l = fmaf(__shfl_sync(0xffffffffu, ml.y, i), f, l);
-#pragma unroll
-            for (int e = 0; e < E; ++e) o[e] = fmaf(x[i][e], f, o[e]);
+            for (int e = 0; e < E; e += 2) y[e / 2] = pack_bf16(o[r][e] * inv, o[r][e + 1] * inv);
+            if constexpr (E == 2) *reinterpret_cast<uint32_t *>(to) = y[0];
+            else if constexpr (E == 4) *reinterpret_cast<uint2 *>(to) = make_uint2(y[0], y[1]);
+            else *reinterpret_cast<uint4 *>(to) = make_uint4(y[0], y[1], y[2], y[3]);
         }
     }
-    if (__any_sync(0xffffffffu, skip)) return;
-    const int group = p.H / p.HK, at = j.row0 + row, node = at / group, g = at % group;
-    __nv_bfloat16 *to = p.o + ((size_t(j.l) * p.T + j.base + node) * p.H + j.hk * group + g) * D + lane * E;
-    const float inv = 1.f / l;
-#pragma unroll
-    for (int e = 0; e < E; e += 2) *reinterpret_cast<uint32_t *>(to + e) = pack_bf16(o[e] * inv, o[e + 1] * inv);
 }
 
 // rows of a unit at most
@@ -723,8 +747,9 @@ template <int D> int launch_width(const AttnParams &p, cudaStream_t st)
             return int(cudaGetLastError());
         });
     if (e != 0) return e;
-    const int blocks = (rows_cap + kJoinWarps - 1) / kJoinWarps;
-    launch(join_kernel<D>, unsigned(grid * blocks), kJoinWarps * 32, 0, st, p, plan, int32_t(blocks));
+    const int needed = (rows_cap + kJoinWarps - 1) / kJoinWarps, blocks = needed < kJoinBlocks ? needed : kJoinBlocks;
+    if (rows_cap <= 16) launch(join_kernel<D, true>, unsigned(grid * blocks), kJoinWarps * 32, 0, st, p, plan, int32_t(blocks));
+    else launch(join_kernel<D, false>, unsigned(grid * blocks), kJoinWarps * 32, 0, st, p, plan, int32_t(blocks));
     return int(cudaGetLastError());
 }
 
