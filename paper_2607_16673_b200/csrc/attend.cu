@@ -43,7 +43,7 @@ template <int DH, bool MANY> struct Cfg {
     static constexpr int Q_ALL = Q_BYTES * (MT / 128) > 4096 * SOFT ? Q_BYTES * (MT / 128) : 4096 * SOFT;
     static constexpr int TILE = N * D * 2;                   // keys or values of a tile
     static constexpr int FIT = (228 * 1024 - Q_ALL) / TILE - (D == 64 ? 1 : 0);                  // tiles in flight or in use
-    static constexpr int KS = FIT / 2, VS = FIT - KS;
+    static constexpr int VS = FIT / 2, KS = FIT - VS;
     static constexpr int OffQ = 0;
     static constexpr int OffRing = Q_ALL;
     static constexpr int OffPar = OffRing + (KS + VS) * TILE;    // int16 parent[kAttnMaxTree]
@@ -312,6 +312,9 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
         uint32_t phase = 0;
         int16_t *par = reinterpret_cast<int16_t *>(smem + C::OffPar);
         auto sync = [&]() { return ok = all_well<SOFT * 32>(ok); };
+        // quotient by the group of less than 2^16 (a unit's rows from the first row of its first node on)
+        const uint32_t inverse = group > 1 ? uint32_t(0xffffffffu / uint32_t(group)) + 1u : 0u;
+        auto by_group = [&](int y) { return group > 1 ? int(__umulhi(uint32_t(y), inverse)) : y; };
         for (uint32_t seg = 0;; ++seg) {
             const bool more = record(seg, r);
             if (!sync() || !more) break;                     // everyone is through with the last segment: its queries, its parents
@@ -320,9 +323,10 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
             const int all = tiles << (two ? 1 : 0);          // items of both groups
             if (threadIdx.x == 0) topo_bad[(seg & 1) ^ 1] = 0;
             {
-                const int chunks = r.rows * (D / 8);
+                const int chunks = r.rows * (D / 8), first = r.row0 / group, ahead = r.row0 - first * group;
+#pragma unroll 2
                 for (int i = threadIdx.x; i < chunks; i += SOFT * 32) {
-                    const int row = i / (D / 8), c = i % (D / 8), at = r.row0 + row, node = at / group, g = at - node * group;
+                    const int row = i / (D / 8), c = i % (D / 8), at = ahead + row, past = by_group(at), node = first + past, g = at - past * group;
                     const int tile = row >> 7, tr = row & 127;
                     copy16(sbase + C::OffQ + tile * C::Q_BYTES + (c >> 3) * (128 * 128) + tr * 128 + (((c & 7) ^ (tr & 7)) << 4),
                            p.q + ((size_t(r.l) * p.T + r.base + node) * p.H + r.hk * group + g) * D + c * 8);
