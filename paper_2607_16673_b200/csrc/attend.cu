@@ -36,6 +36,9 @@ template <int DH, bool MANY> struct Cfg {
     static constexpr int BUFS = LANES == 1 ? 3 : MANY ? 4 : 2;
     static constexpr int MT = MANY && LANES == 2 ? 256 : 128;
     static constexpr int kEnds = N == 128 ? 5 : D == 256 ? 8 : 10;          // a unit's beginning and end in tiles: some 15000 cycles
+    // 384 keys (512) and 768: 20 trees of 9..40 nodes behind 10..300 tokens 26.7 -> 18.9 us, one tree of 64 at 256 columns behind 3000
+    // 55.5 -> 37.7, of 32 at 128 columns behind 1000 24.2 -> 20.4, large calls as they were
+    static constexpr int kPiece = D == 256 ? 8 : 3 * (128 / N), kWhole = 6 * (128 / N);
     static constexpr bool kMend = true;
     static constexpr int SOFT = 4 * LANES;                   // softmax warps; then keys, scores, products with V, mending of V, schedule, values
     static constexpr int THREADS = (SOFT + 6) * 32;
@@ -198,7 +201,7 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
 
     if (warp == SOFT) {
         // ------------------------------------------------------------------------------- keys and values, by TMA
-        x.load<0>(maps, box_rows);
+        x.template load<0>(maps, box_rows);
     } else if (warp == SOFT + 1) {
         // ------------------------------------------------------------------------------- scores
         const uint32_t id_s = make_idesc_bf16(N);
@@ -303,7 +306,7 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
         // ------------------------------------------------------------------------------- schedule
         x.schedule();
     } else if (warp == SOFT + 5) {
-        x.load<1>(maps, box_rows);
+        x.template load<1>(maps, box_rows);
     } else {
         // ------------------------------------------------------------------------------- softmax, and what is written
         const int wg = warp >> 2, quad = warp & 3, trow = quad * 32 + lane;      // lane of TMEM: row of this group's tile
@@ -738,19 +741,30 @@ template <int D> int launch_width(const AttnParams &p, cudaStream_t st)
     };
     int e = opt_in();
     if (e != 0) return e;
-    if (attend_few_rows(long(p.max_nodes) * (p.H / p.HK)) > 0)
+    // whether no unit can be cut, as far as the host can tell: the table holds too little
+    bool whole;
+    auto never_cut = [&](int keys, int most, int weight) {
+        return ((long(p.max_pages) * page + keys - 1) / keys + (p.max_nodes + keys - 1) / keys) * weight <= most;
+    };
+    if (attend_few_rows(long(p.max_nodes) * (p.H / p.HK)) > 0) {
+        whole = never_cut(D == 256 ? 64 : 128, kFewWhole, 1);
         e = go(D == 256 ? 64 : 128, [&](int box) { return launch_attend_few(p, D, maps, plan, box, grid, st); });
-    else if (D == 256 || rows_cap > 128)
-        e = go(64, [&](int box) {
-            launch(attend_kernel<D, true>, grid, Cfg<D, true>::THREADS, Cfg<D, true>::Bytes, st, maps, p, plan, int32_t(box));
+    } else if (D == 256 || rows_cap > 128) {
+        using C = Cfg<D, true>;
+        whole = never_cut(C::N, C::kWhole, C::MT == 256 ? 2 : 1);
+        e = go(C::N, [&](int box) {
+            launch(attend_kernel<D, true>, grid, C::THREADS, C::Bytes, st, maps, p, plan, int32_t(box));
             return int(cudaGetLastError());
         });
-    else if constexpr (D != 256)
-        e = go(128, [&](int box) {
-            launch(attend_kernel<D, false>, grid, Cfg<D, false>::THREADS, Cfg<D, false>::Bytes, st, maps, p, plan, int32_t(box));
+    } else {
+        using C = Cfg<D == 256 ? 128 : D, false>;            // (D = 256 went above)
+        whole = never_cut(C::N, C::kWhole, 1);
+        e = go(C::N, [&](int box) {
+            launch(attend_kernel<C::D, false>, grid, C::THREADS, C::Bytes, st, maps, p, plan, int32_t(box));
             return int(cudaGetLastError());
         });
-    if (e != 0) return e;
+    }
+    if (e != 0 || whole) return e;                           // 2.5 us for a join that finds nothing to do
     const int needed = (rows_cap + kJoinWarps - 1) / kJoinWarps, blocks = needed < kJoinBlocks ? needed : kJoinBlocks;
     if (rows_cap <= 16) launch(join_kernel<D, true>, unsigned(grid * blocks), kJoinWarps * 32, 0, st, p, plan, int32_t(blocks));
     else launch(join_kernel<D, false>, unsigned(grid * blocks), kJoinWarps * 32, 0, st, p, plan, int32_t(blocks));

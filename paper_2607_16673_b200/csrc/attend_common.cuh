@@ -13,6 +13,7 @@ using namespace tc;
 constexpr int kMaxCtas = 160;            // pieces of the list at most (148 SMs)
 constexpr int kRecords = 4;              // ring of segment records
 constexpr int kFlagRing = 8;
+constexpr int kFewWhole = 4;             // tiles of a unit of few rows that is never cut (6 chains behind 10..300 tokens 17.9 -> 15.4 us)
 
 // A piece of one unit: key tiles t0 .. t1-1, of which the first `ct` of the unit are the cache's.
 struct Rec {
@@ -133,6 +134,12 @@ template <class C> __device__ __forceinline__ int row_tiles(const Seq &s, int gr
 {
     return (s.n * group + C::MT - 1) / C::MT;     // (at most 8192 nodes and 65536 heads)
 }
+template <class C> __device__ __forceinline__ int longest_unit(const Seq &s, int group)
+{
+    // (the last full row tile sees most)
+    const int tiles = s.ct + (s.n + C::N - 1) / C::N;
+    return tiles * (C::MT == 256 && s.n * group > 128 ? 2 : 1);
+}
 // cost of one layer and key head
 template <class C> __device__ __forceinline__ long head_cost(const Seq &s, int group)
 {
@@ -152,7 +159,7 @@ struct Maps {
     CUtensorMap k, v, k_draft, v_draft;
 };
 
-// A CTA's view of the work.  C: N keys a tile, D columns, MT rows of a unit, kEnds, KS and VS slots of TILE bytes
+// A CTA's view of the work.  C: N keys a tile, D columns, MT rows of a unit, kEnds, kPiece and kWhole of the schedule, KS and VS slots of TILE bytes
 // at OffRing (keys, then values), barriers from OffBars.
 // (A barrier has two parities: whoever waits on one waits for all its phases in turn.  So keys and values have rings of their
 // own, and where C::kMend, values that are looked over before they are used land on barriers of their own.)
@@ -306,18 +313,24 @@ template <class C> struct Cta {
             return head_cost<C>(s, group);
         };
         long total = 0, first = 0;
+        int longest = 0;                                     // unit, its ends aside
 #pragma unroll 1
         for (int b0 = 0; b0 < p.B; b0 += 32) {
             const long c = fetch(b0);
             if (b0 == 0) first = c;
             if (s.fault && cta == 0) atomicOr(p.status, s.fault);
             total += c;
+            if (c > 0) longest = max(longest, longest_unit<C>(s, group));
         }
+        longest = int(__reduce_max_sync(0xffffffffu, unsigned(longest)));
 #pragma unroll
         for (int i = 16; i > 0; i /= 2) total += __shfl_xor_sync(0xffffffffu, total, i);
         total *= heads;
-        // (a piece is at least one tile long, so that every CTA between a unit's first and last has some of it)
-        const int pieces = int(min(long(grid), max(1L, total / (C::MT == 256 ? 2 : 1))));
+        // A piece is at least kPiece long: at least one tile, so that every CTA between a unit's first and last has some of it, and
+        // more where rows make their joining dear.  Units of up to kWhole are not cut at all, but go to the CTA in whose piece they
+        // begin.
+        const bool whole = longest <= C::kWhole;
+        const int pieces = int(min(long(grid), max(1L, total / C::kPiece)));
         const long per = quotient(total, pieces), extra = total - per * pieces;
         const long begin = cta * per + min(long(cta), extra), end = cta < pieces ? begin + per + (cta < extra ? 1 : 0) : begin;
         long at = 0;                                         // place in the list of the sequence looked at
@@ -359,8 +372,9 @@ template <class C> struct Cta {
                         // a tile is whose piece its beginning is in
                         auto tile_from = [&](long x) { return x <= tiles_at ? 0 : int(min(long(ut), (x - tiles_at + w - 1) >> (w - 1))); };
                         Rec x{};
-                        x.t0 = tile_from(begin);
-                        x.t1 = tile_from(end);
+                        const bool own = tiles_at - C::kEnds >= begin;           // (it is before the end)
+                        x.t0 = whole ? 0 : tile_from(begin);
+                        x.t1 = whole ? (own ? ut : 0) : tile_from(end);
                         if (x.t1 <= x.t0) continue;
                         x.l = hd / p.HK; x.b = b0 + i; x.hk = hd - x.l * p.HK; x.base = q.base; x.n = q.n; x.len = q.len;
                         x.row0 = m * C::MT;
