@@ -411,7 +411,9 @@ int speca_norm_rope(const speca_attn_dims *dims,
 
 /* Verification by an attention layer: node t attends the committed rows 0 .. kv_len[b]-1 of its sequence, its ancestors in
  * the draft and itself.  Scores, softmax and sums in fp32; weights are rounded to bf16 for the product with v, and o
- * once at the end.  A key or value that is not finite reaches the nodes that attend it and no others. */
+ * once at the end.  A key or value that is not finite reaches the nodes that attend it and no others.  The result is the same
+ * for the same call, whatever else runs.  What the workspace holds before and after a call does not matter; calls that may
+ * run at the same time need one each.  After SPECA_STATUS_TIMEOUT o is undefined. */
 size_t speca_attn_workspace_bytes(const speca_attn_dims *dims);
 int speca_attend_tree(const speca_attn_dims *dims, const uint16_t *q, const uint16_t *k, const uint16_t *v,
                       const int32_t *node_offsets, int32_t total_nodes, const int32_t *parent_or_null,
@@ -436,8 +438,8 @@ int speca_commit_kv(const speca_attn_dims *dims, uint16_t *k_cache, uint16_t *v_
 /* Copies page src[i] onto page dst[i], i < n_copies, in every layer, keys and values: the page a forked sequence goes on
  * writing (full pages need no copy, they are shared).  src, dst int32 [n_copies], device.  A source may be named often.
  * Copies are unordered, so a pair whose dst is out of range, is another pair's dst, or is any pair's src is reported
- * (STATUS_BAD_PAGE) and not made, and so is one whose src is out of range; the others are.  Of dims only n_layers,
- * kv_heads, d_head, page_size and n_pages matter. */
+ * (STATUS_BAD_PAGE) and not made, and so is one whose src is out of range; the others are.  dims is checked as in every
+ * call; n_layers, kv_heads, d_head, page_size and n_pages of it are used. */
 int speca_copy_pages(const speca_attn_dims *dims, uint16_t *k_cache, uint16_t *v_cache,
                      const int32_t *src, const int32_t *dst, int32_t n_copies, int32_t *status_word, void *stream);
 

@@ -24,7 +24,7 @@ constexpr float kSlack = 8.f;            // binary digits a maximum may grow by 
 template <int DH> struct Few {
     static constexpr int D = DH;
     static constexpr int N = D == 256 ? 64 : 128;
-    static constexpr int LANES = 1, MT = kRows, kEnds = 3, kPiece = 1, kWhole = kFewWhole;
+    static constexpr int MT = kRows, kEnds = 3, kPiece = 1, kWhole = kFewWhole;
     static constexpr bool kMend = false;
     static constexpr int THREADS = (kConsumers + 3) * 32;
     static constexpr int OC = D < 128 ? D : 128, CH = D / OC;
