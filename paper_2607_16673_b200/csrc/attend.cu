@@ -175,7 +175,8 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
     auto bar = [&](int i) { return x.bar(i); };
     volatile int *const abort_flag = x.abort_flag, *const topo_bad = x.topo_bad;
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + C::OffMisc + 4);
-    const int warp = x.warp, lane = x.lane, group = x.group, cta = blockIdx.x;
+    const int warp = x.warp, lane = x.lane, cta = blockIdx.x;
+    const Group group = x.group;
 
     if (warp == 0) {
         x.init(SOFT + 5, 1);
@@ -315,9 +316,6 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
         uint32_t phase = 0;
         int16_t *par = reinterpret_cast<int16_t *>(smem + C::OffPar);
         auto sync = [&]() { return ok = all_well<SOFT * 32>(ok); };
-        // quotient by the group of less than 2^16 (a unit's rows from the first row of its first node on)
-        const uint32_t inverse = group > 1 ? uint32_t(0xffffffffu / uint32_t(group)) + 1u : 0u;
-        auto by_group = [&](int y) { return group > 1 ? int(__umulhi(uint32_t(y), inverse)) : y; };
         for (uint32_t seg = 0;; ++seg) {
             const bool more = record(seg, r);
             if (!sync() || !more) break;                     // everyone is through with the last segment: its queries, its parents
@@ -326,13 +324,13 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
             const int all = tiles << (two ? 1 : 0);          // items of both groups
             if (threadIdx.x == 0) topo_bad[(seg & 1) ^ 1] = 0;
             {
-                const int chunks = r.rows * (D / 8), first = r.row0 / group, ahead = r.row0 - first * group;
+                const int chunks = r.rows * (D / 8), first = group.over(r.row0), ahead = r.row0 - first * group.n;
 #pragma unroll 2
                 for (int i = threadIdx.x; i < chunks; i += SOFT * 32) {
-                    const int row = i / (D / 8), c = i % (D / 8), at = ahead + row, past = by_group(at), node = first + past, g = at - past * group;
+                    const int row = i / (D / 8), c = i % (D / 8), at = ahead + row, past = group.over(at), node = first + past, g = at - past * group.n;
                     const int tile = row >> 7, tr = row & 127;
                     copy16(sbase + C::OffQ + tile * C::Q_BYTES + (c >> 3) * (128 * 128) + tr * 128 + (((c & 7) ^ (tr & 7)) << 4),
-                           p.q + ((size_t(r.l) * p.T + r.base + node) * p.H + r.hk * group + g) * D + c * 8);
+                           p.q + ((size_t(r.l) * p.T + r.base + node) * p.H + r.hk * group.n + g) * D + c * 8);
                 }
                 copy16_wait();
                 fence_proxy_async();
@@ -354,7 +352,7 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
             }
             const int row = (two ? wg * 128 : 0) + trow;     // row of the unit
             const bool live = (two ? wg * 128 : 0) + quad * 32 < r.rows;     // the warp has rows
-            const int at = r.row0 + (row < r.rows ? row : 0), node = at / group, g = at - node * group;
+            const int at = r.row0 + (row < r.rows ? row : 0), node = group.over(at), g = at - node * group.n;
             float m = -INFINITY, l = 0.f;
             const int mine = LANES == 2 ? (all + 1 - wg) / 2 : all;          // items of this group
             uint32_t uses = phase;                           // parities that its own items have turned
@@ -507,7 +505,7 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
                 const int c_lo = merge ? wg * (D / 2) : 0, c_hi = merge ? c_lo + D / 2 : D;
                 const float inv = 1.f / ll;
                 float *sums = r.slot >= 0 ? slot_sums(plan, cta, r.slot) : nullptr;
-                __nv_bfloat16 *out = p.o + ((size_t(r.l) * p.T + r.base + node) * p.H + r.hk * group + g) * D;
+                __nv_bfloat16 *out = p.o + ((size_t(r.l) * p.T + r.base + node) * p.H + r.hk * group.n + g) * D;
                 const bool write = row < r.rows && !skip;
                 if (sums == nullptr) { f0 *= inv; f1 *= inv; }
                 // Through shared memory (this group's queries have been used), so that a row is written in whole lines: straight

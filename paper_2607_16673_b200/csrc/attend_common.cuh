@@ -96,6 +96,20 @@ __device__ __forceinline__ bool not_finite(uint32_t pair)
 // ---------------------------------------------------------------------------------------------------------------
 // The list of tiles
 // ---------------------------------------------------------------------------------------------------------------
+// Query heads to a key head, and quotients of numbers >= 0 by them without a division (some forty instructions, and a prompt's
+// list takes hundreds): the inverse is rounded up, so the product's high half is the quotient or one more.
+struct Group {
+    int n;
+    uint32_t inverse;
+    __device__ __forceinline__ explicit Group(int heads) : n(heads), inverse(heads > 1 ? 0xffffffffu / uint32_t(heads) + 1u : 0u) {}
+    __device__ __forceinline__ int over(int y) const
+    {
+        if (n == 1) return y;
+        const int q = int(__umulhi(uint32_t(y), inverse));
+        return q - (q * n > y);
+    }
+};
+
 struct Seq {
     int base, n, len, ct, fault;
 };
@@ -111,43 +125,43 @@ template <class C> __device__ __forceinline__ Seq sequence(const AttnParams &p, 
     return s;
 }
 // draft nodes that the rows of row tile m can see
-template <int MT> __device__ __forceinline__ int nodes_seen(int n, int group, int m)
+template <int MT> __device__ __forceinline__ int nodes_seen(int n, const Group &group, int m)
 {
-    return min(n, ((m + 1) * MT - 1) / group + 1);
+    return min(n, group.over((m + 1) * MT - 1) + 1);
 }
-template <class C> __device__ __forceinline__ long unit_tiles(const Seq &s, int group, int m)
+template <class C> __device__ __forceinline__ long unit_tiles(const Seq &s, const Group &group, int m)
 {
     return s.ct + (nodes_seen<C::MT>(s.n, group, m) + C::N - 1) / C::N;
 }
 // Cost of a unit, in tiles: its own (twice as many where two row tiles share the keys) and what begins and ends it, queries in,
 // sums out, the pipeline filled and drained.  Pieces are equal in this measure: with tiles alone counted, CTAs that got many
 // short sequences took up to twice as long as the others.
-template <class C> __device__ __forceinline__ int tile_cost(const Seq &s, int group, int m)
+template <class C> __device__ __forceinline__ int tile_cost(const Seq &s, const Group &group, int m)
 {
-    return C::MT == 256 && s.n * group - m * C::MT > 128 ? 2 : 1;
+    return C::MT == 256 && s.n * group.n - m * C::MT > 128 ? 2 : 1;
 }
-template <class C> __device__ __forceinline__ long unit_cost(const Seq &s, int group, int m)
+template <class C> __device__ __forceinline__ long unit_cost(const Seq &s, const Group &group, int m)
 {
     return unit_tiles<C>(s, group, m) * tile_cost<C>(s, group, m) + C::kEnds;
 }
-template <class C> __device__ __forceinline__ int row_tiles(const Seq &s, int group)
+template <class C> __device__ __forceinline__ int row_tiles(const Seq &s, const Group &group)
 {
-    return (s.n * group + C::MT - 1) / C::MT;     // (at most 8192 nodes and 65536 heads)
+    return (s.n * group.n + C::MT - 1) / C::MT;             // (at most 8192 nodes and 4096 heads)
 }
-template <class C> __device__ __forceinline__ int longest_unit(const Seq &s, int group)
+template <class C> __device__ __forceinline__ int longest_unit(const Seq &s, const Group &group)
 {
     // (the last full row tile sees most)
     const int tiles = s.ct + (s.n + C::N - 1) / C::N;
-    return tiles * (C::MT == 256 && s.n * group > 128 ? 2 : 1);
+    return tiles * (C::MT == 256 && s.n * group.n > 128 ? 2 : 1);
 }
 // cost of one layer and key head
-template <class C> __device__ __forceinline__ long head_cost(const Seq &s, int group)
+template <class C> __device__ __forceinline__ long head_cost(const Seq &s, const Group &group)
 {
     long sum = 0;
-    for (int m = 0; m < row_tiles<C>(s, group); ++m) sum += unit_cost<C>(s, group, m);
+    const int tiles = row_tiles<C>(s, group);
+    for (int m = 0; m < tiles; ++m) sum += unit_cost<C>(s, group, m);
     return sum;
 }
-
 
 // a / b of positive numbers: a division of 64 bits is a call of some hundred instructions, in front of the first tile
 __device__ __forceinline__ long quotient(long a, long b)
@@ -159,8 +173,8 @@ struct Maps {
     CUtensorMap k, v, k_draft, v_draft;
 };
 
-// A CTA's view of the work.  C: N keys a tile, D columns, MT rows of a unit, kEnds, kPiece and kWhole of the schedule, KS and VS slots of TILE bytes
-// at OffRing (keys, then values), barriers from OffBars.
+// A CTA's view of the work.  C: N keys a tile, D columns, MT rows of a unit, kEnds, kPiece and kWhole of the schedule, KS and VS
+// slots of TILE bytes at OffRing (keys, then values), barriers from OffBars.
 // (A barrier has two parities: whoever waits on one waits for all its phases in turn.  So keys and values have rings of their
 // own, and where C::kMend, values that are looked over before they are used land on barriers of their own.)
 template <class C> struct Cta {
@@ -169,7 +183,8 @@ template <class C> struct Cta {
     const Plan &plan;
     uint8_t *smem;
     uint32_t sbase;
-    int warp, lane, group;
+    int warp, lane;
+    Group group;
     volatile int *abort_flag, *topo_bad, *page_bad, *value_bad;      // topo_bad [2], the others [kFlagRing]: 1 + segment number
     uint32_t lead;
     bool ok;
@@ -211,7 +226,7 @@ template <class C> struct Cta {
     // whether every row of the unit attends all keys of tile t (of a chain's draft those below its first node)
     __device__ __forceinline__ bool all_seen(const Rec &r, int t) const
     {
-        return t < r.ct || (p.parent == nullptr && (t - r.ct + 1) * N <= r.row0 / group + 1);
+        return t < r.ct || (p.parent == nullptr && (t - r.ct + 1) * N <= group.over(r.row0) + 1);
     }
     __device__ __forceinline__ bool to_mend(const Rec &r, int t) const
     {
@@ -293,8 +308,8 @@ template <class C> struct Cta {
         uint32_t seg = 0;
         auto put = [&](const Rec &x) {
             // the unit's queries are asked into L2 while the segments before it are worked on
-            for (int node = x.row0 / group + lane; node * group < x.row0 + x.rows; node += 32)
-                prefetch_l2(p.q + ((size_t(x.l) * p.T + x.base + node) * p.H + x.hk * group) * D, uint32_t(group) * D * 2);
+            for (int node = group.over(x.row0) + lane; node * group.n < x.row0 + x.rows; node += 32)
+                prefetch_l2(p.q + ((size_t(x.l) * p.T + x.base + node) * p.H + x.hk * group.n) * D, uint32_t(group.n) * D * 2);
             ok = seg < kRecords || wait_fast(bar(C::kRecEmpty + (seg % kRecords)), ((seg / kRecords) & 1) ^ 1, abort_flag);
             if (!ok) return;
             if (lane == 0) {
@@ -378,7 +393,7 @@ template <class C> struct Cta {
                         if (x.t1 <= x.t0) continue;
                         x.l = hd / p.HK; x.b = b0 + i; x.hk = hd - x.l * p.HK; x.base = q.base; x.n = q.n; x.len = q.len;
                         x.row0 = m * C::MT;
-                        x.rows = min(C::MT, q.n * group - x.row0);
+                        x.rows = min(C::MT, q.n * group.n - x.row0);
                         x.ct = q.ct;
                         x.nodes = nodes_seen<C::MT>(q.n, group, m);
                         x.slot = x.t0 == 0 && x.t1 == ut ? -1 : x.t0 == 0 ? 1 : 0;

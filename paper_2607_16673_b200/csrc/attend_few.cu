@@ -85,7 +85,8 @@ attend_few_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, in
         if (threadIdx.x == 0) atomicOr(p.status, SPECA_STATUS_TIMEOUT);
         return;
     }
-    const int warp = x.warp, lane = x.lane, group = x.group, cta = blockIdx.x;
+    const int warp = x.warp, lane = x.lane, cta = blockIdx.x;
+    const Group group = x.group;
     if (warp == 0) {
         x.init(kConsumers + 2, kConsumers);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -112,8 +113,8 @@ attend_few_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, in
             const bool tree = p.parent != nullptr && r.t1 > r.ct;
             if (threadIdx.x == 0) x.topo_bad[(seg & 1) ^ 1] = 0;
             for (int i = threadIdx.x; i < r.rows * (D / 8); i += kConsumers * 32) {
-                const int row = i / (D / 8), c = i % (D / 8), at = r.row0 + row, node = at / group, g = at - node * group;
-                copy16(q_at + tile_offset<D>(row, c), p.q + ((size_t(r.l) * p.T + r.base + node) * p.H + r.hk * group + g) * D + c * 8);
+                const int row = i / (D / 8), c = i % (D / 8), at = r.row0 + row, node = group.over(at), g = at - node * group.n;
+                copy16(q_at + tile_offset<D>(row, c), p.q + ((size_t(r.l) * p.T + r.base + node) * p.H + r.hk * group.n + g) * D + c * 8);
             }
             if (tree) {                                      // (at most as many nodes as rows)
                 int bad = 0;
@@ -137,7 +138,7 @@ attend_few_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, in
             for (int h = 0; h < 2; ++h) {
                 live[h] = row0 + 8 * h < r.rows;
                 if (!live[h] || r.t1 <= r.ct) continue;
-                for (int a = (r.row0 + row0 + 8 * h) / group; a >= 0; a = tree ? int(par[a]) : a - 1) seen[h] |= 1u << a;
+                for (int a = group.over(r.row0 + row0 + 8 * h); a >= 0; a = tree ? int(par[a]) : a - 1) seen[h] |= 1u << a;
             }
             float o[OC / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
@@ -269,8 +270,8 @@ attend_few_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, in
             const bool put_back = x.value_bad[seg % kFlagRing] == int(seg) + 1;
             float *sums = r.slot >= 0 ? slot_sums(plan, cta, r.slot) : nullptr;
             auto out_of = [&](int row) {
-                const int at = r.row0 + row, node = at / group, g = at - node * group;
-                return p.o + ((size_t(r.l) * p.T + r.base + node) * p.H + r.hk * group + g) * D;
+                const int at = r.row0 + row, node = group.over(at), g = at - node * group.n;
+                return p.o + ((size_t(r.l) * p.T + r.base + node) * p.H + r.hk * group.n + g) * D;
             };
             if (sums != nullptr && threadIdx.x == 0) reinterpret_cast<int *>(sums + size_t(plan.rows_cap) * (D + 2))[0] = skip;
 #pragma unroll
@@ -316,7 +317,7 @@ attend_few_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, in
                 for (int u = threadIdx.x; u < r.rows * D; u += kConsumers * 32) {
                     // (column u % D of a row; what other threads have written of it is behind the last sync)
                     const int row = u / D, col = u % D;
-                    for (int a = (r.row0 + row) / group; a >= 0; a = tree ? int(par[a]) : a - 1) {
+                    for (int a = group.over(r.row0 + row); a >= 0; a = tree ? int(par[a]) : a - 1) {
                         const float y = __bfloat162float(p.v[((size_t(r.l) * p.T + r.base + a) * p.HK + r.hk) * D + col]);
                         if (isfinite(y)) continue;
                         if (sums == nullptr) out_of(row)[col] = __float2bfloat16_rn(__bfloat162float(out_of(row)[col]) + y);
