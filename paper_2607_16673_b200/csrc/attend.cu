@@ -22,7 +22,8 @@ constexpr float kSlack = 8.f;            // binary digits a maximum may grow by 
 
 // D <= 128: two softmax groups of 128 rows, each with an O of its own.  A unit of at most 128 rows has its even key tiles in one
 // and the odd ones in the other, joined at the end; a larger one has a row tile in each, over the same keys.  D = 256: O alone
-// takes half of TMEM, and there is one group.  P takes the first half of the columns of its S.  One warp asks for scores, another
+// takes half of TMEM, and there is one group; its queries have a quarter of TMEM, so that a tile's scores do not read 64 KB of
+// shared memory once more and the rings have room for one tile more.  P takes the first half of the columns of its S.  One warp asks for scores, another
 // for the products with V, so that neither's waits hold the other up (a loop over one item takes 1200 cycles beside its 12
 // products where one warp does both).
 // MANY: units of more than 128 rows.  Products and softmax bound these: tiles of 64 keys leave room for a second buffer of S in
@@ -33,7 +34,7 @@ template <int DH, bool MANY> struct Cfg {
     static constexpr int D = DH;
     static constexpr int LANES = D == 256 ? 1 : 2;
     static constexpr int N = MANY || D == 256 ? 64 : 128;
-    static constexpr int BUFS = LANES == 1 ? 3 : MANY ? 4 : 2;
+    static constexpr int BUFS = LANES == 2 && MANY ? 4 : 2;
     static constexpr int MT = MANY && LANES == 2 ? 256 : 128;
     static constexpr int kEnds = N == 128 ? 5 : D == 256 ? 8 : 10;          // a unit's beginning and end in tiles: some 15000 cycles
     // 384 keys (512) and 768: 20 trees of 9..40 nodes behind 10..300 tokens 26.7 -> 18.9 us, one tree of 64 at 256 columns behind 3000
@@ -43,7 +44,7 @@ template <int DH, bool MANY> struct Cfg {
     static constexpr int SOFT = 4 * LANES;                   // softmax warps; then keys, scores, products with V, mending of V, schedule, values
     static constexpr int THREADS = (SOFT + 6) * 32;
     static constexpr int Q_BYTES = 128 * D * 2;              // queries of a row tile; at a unit's end sums on their way, 4096 bytes a warp
-    static constexpr int Q_ALL = Q_BYTES * (MT / 128) > 4096 * SOFT ? Q_BYTES * (MT / 128) : 4096 * SOFT;
+    static constexpr int Q_ALL = D < 256 && Q_BYTES * (MT / 128) > 4096 * SOFT ? Q_BYTES * (MT / 128) : 4096 * SOFT;
     static constexpr int TILE = N * D * 2;                   // keys or values of a tile
     static constexpr int FIT = (228 * 1024 - Q_ALL) / TILE - (D == 64 ? 1 : 0);                  // tiles in flight or in use
     static constexpr int VS = FIT / 2, KS = FIT - VS;
@@ -63,7 +64,7 @@ template <class C> constexpr bool fits() { return C::Bytes <= 232448 && C::KS >=
 static_assert(fits<Cfg<64, false>>() && fits<Cfg<64, true>>() && fits<Cfg<128, false>>() && fits<Cfg<128, true>>() && fits<Cfg<256, true>>(),
               "shared memory of a CTA");
 
-constexpr int kTmemCols = 512, kOCol = 256;                  // S (P) buffers from 0, N columns each, O from column 256
+constexpr int kTmemCols = 512, kQCol = 128, kOCol = 256;     // S (P) buffers from 0, N columns each, at D = 256 the queries, O
 
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float *r)
 {
@@ -197,7 +198,7 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
     auto valid_of = [&](const Rec &r, int t) { return x.valid_of(r, t); };
     // Buffer of item i of a segment.  Every use of a buffer is one phase of its three barriers (scores there, weights there,
     // weights used); a role keeps the parity of the next one, a bit a buffer.
-    auto buffer = [](int i) { return LANES == 2 ? i & (BUFS - 1) : i % 3; };
+    auto buffer = [](int i) { return i & (BUFS - 1); };
     Rec r;
 
     if (warp == SOFT) {
@@ -224,7 +225,10 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
                 const uint64_t qd = make_desc(sbase + C::OffQ + (two ? (i & 1) * C::Q_BYTES : 0)), kd = make_desc_k(sbase + C::OffRing + s * C::TILE, 16 * D);
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k)
-                    mma_bf16(tmem + buf * N, qd + uint64_t(((k >> 2) * (128 * 128) + (k & 3) * 32) >> 4),
+                    if constexpr (D == 256)
+                        mma_bf16_ts(tmem + buf * N, tmem + kQCol + 8 * k, kd + uint64_t(((k >> 2) * 1024 + (k & 3) * 32) >> 4), id_s, k != 0, lead);
+                    else
+                        mma_bf16(tmem + buf * N, qd + uint64_t(((k >> 2) * (128 * 128) + (k & 3) * 32) >> 4),
                              kd + uint64_t(((k >> 2) * 1024 + (k & 3) * 32) >> 4), id_s, k != 0, lead);
                 mma_commit(bar(C::kSFull + buf), lead);
                 if (!two || (i & 1)) mma_commit(bar(C::kKEmpty + s), lead);
@@ -323,20 +327,42 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
             const int tiles = r.t1 - r.t0;
             const int all = tiles << (two ? 1 : 0);          // items of both groups
             if (threadIdx.x == 0) topo_bad[(seg & 1) ^ 1] = 0;
-            {
-                const int chunks = r.rows * (D / 8), first = group.over(r.row0), ahead = r.row0 - first * group.n;
+            const int first = group.over(r.row0), ahead = r.row0 - first * group.n;
+            const __nv_bfloat16 *queries = p.q + ((size_t(r.l) * p.T + r.base) * p.H + r.hk * group.n) * D;
+            if constexpr (D == 256) {
+                if (quad * 32 < r.rows) {
+                    const int at = ahead + trow, past = group.over(at);
+                    const uint4 *from = reinterpret_cast<const uint4 *>(queries + (size_t(first + past) * p.H + (at - past * group.n)) * D);
+#pragma unroll 1
+                    for (int c = 0; c < 4; c += 2) {
+                        uint4 y[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) y[e] = trow < r.rows ? from[8 * c + e] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) {
+                            const uint32_t z[16] = {y[4 * h].x, y[4 * h].y, y[4 * h].z, y[4 * h].w, y[4 * h + 1].x, y[4 * h + 1].y, y[4 * h + 1].z,
+                                                    y[4 * h + 1].w, y[4 * h + 2].x, y[4 * h + 2].y, y[4 * h + 2].z, y[4 * h + 2].w,
+                                                    y[4 * h + 3].x, y[4 * h + 3].y, y[4 * h + 3].z, y[4 * h + 3].w};
+                            tmem_st16(tq + kQCol + 32 * c + 16 * h, z);
+                        }
+                    }
+                    tmem_st_wait();
+                    tc_fence_before();
+                }
+            } else {
+                const int chunks = r.rows * (D / 8);
 #pragma unroll 2
                 for (int i = threadIdx.x; i < chunks; i += SOFT * 32) {
-                    const int row = i / (D / 8), c = i % (D / 8), at = ahead + row, past = group.over(at), node = first + past, g = at - past * group.n;
+                    const int row = i / (D / 8), c = i % (D / 8), at = ahead + row, past = group.over(at);
                     const int tile = row >> 7, tr = row & 127;
                     copy16(sbase + C::OffQ + tile * C::Q_BYTES + (c >> 3) * (128 * 128) + tr * 128 + (((c & 7) ^ (tr & 7)) << 4),
-                           p.q + ((size_t(r.l) * p.T + r.base + node) * p.H + r.hk * group.n + g) * D + c * 8);
+                           queries + (size_t(first + past) * p.H + (at - past * group.n)) * D + c * 8);
                 }
                 copy16_wait();
                 fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(C::kQFull));
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(C::kQFull));
             if (p.parent != nullptr && r.t1 > r.ct) {        // (a piece without draft keys is joined with one that looks)
                 int bad = 0;
                 for (int i = threadIdx.x; i < r.n; i += SOFT * 32) {
