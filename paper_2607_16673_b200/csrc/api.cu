@@ -176,6 +176,7 @@ void speca_test_withhold_first_load(int on)
 {
     factorized_set_withhold(on);
     effective_set_withhold(on);
+    attend_set_withhold(on);
 }
 
 /* Test hook, deliberately absent from speca.h: speca_commit hands accepted paths of six to eight nodes to its

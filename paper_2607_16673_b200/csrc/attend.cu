@@ -802,8 +802,13 @@ size_t attend_workspace_bytes(const speca_attn_dims *d)
     return align256(sizeof(Join) * kMaxCtas) + 2 * kMaxCtas * slot_bytes(unit_rows(d->max_nodes, d->heads / d->kv_heads, d->d_head), d->d_head);
 }
 
-int launch_attend(const AttnParams &p, int d_head, cudaStream_t st)
+static int g_withhold_first_load = 0;
+void attend_set_withhold(int on) { g_withhold_first_load = on; }
+
+int launch_attend(const AttnParams &call, int d_head, cudaStream_t st)
 {
+    AttnParams p = call;
+    p.withhold_first_load = g_withhold_first_load;
     if (d_head == 64) return launch_width<64>(p, st);
     if (d_head == 128) return launch_width<128>(p, st);
     return launch_width<256>(p, st);

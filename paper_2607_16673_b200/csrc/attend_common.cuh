@@ -276,6 +276,7 @@ template <class C> struct Cta {
                 }
                 const int s = n % SLOTS;
                 if (!(ok = wait_fast(bar((KV ? C::kVEmpty : C::kKEmpty) + s), ((n / SLOTS) & 1) ^ 1, abort_flag))) break;
+                if (KV == 0 && n == 0 && p.withhold_first_load && blockIdx.x == 0) continue;
                 const int valid = valid_of(r, t);
                 const uint32_t full = bar((KV == 0 ? C::kKFull : to_mend(r, t) ? C::kVRaw : C::kVFull) + s);
                 const uint32_t dst = sbase + C::OffRing + (KV ? KS + s : s) * C::TILE;

@@ -276,3 +276,22 @@ def test_refusals_of_the_binding_name_the_argument():
     with pytest.raises(speca.SpecaError, match="inv_freq"):
         speca.norm_rope(a.dims, a.q, a.k, None, None, 1e-6, freq, 32, False, 1.0, a.node_offsets, a.T, a.parent, a.kv_len, a.o,
                         torch.empty_like(a.k), a.status)
+
+
+@pytest.mark.parametrize("H,HK,d,n", [(4, 4, 64, 4), (8, 2, 128, 20), (8, 1, 128, 40), (16, 2, 256, 9)])
+def test_a_wait_that_runs_out_is_reported(H, HK, d, n):
+    """A CTA whose first keys never come gives up after its bounded wait, says so and leaves; the next call is as ever."""
+    a = Attn(10, 1, H, HK, d, 16, [300, 40], [synth.random_tree_parent(n, 8, 4, np.random.default_rng(n)), synth.chain_parent(n)])
+    hook = speca.lib().speca_test_withhold_first_load
+    hook(1)
+    try:
+        a.attend()
+        torch.cuda.synchronize()
+    finally:
+        hook(0)
+    assert a.status_value() & speca.STATUS_TIMEOUT
+    a.status.zero_()
+    a.o.fill_(7)
+    a.attend()
+    assert a.status_value() == 0
+    a.check()
