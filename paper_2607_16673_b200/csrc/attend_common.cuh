@@ -121,7 +121,7 @@ template <class C> __device__ __forceinline__ Seq sequence(const AttnParams &p, 
     s.len = p.kv_len[b];
     if (s.len < 0 || (s.len >> p.page_shift) > p.max_pages || s.len > p.max_pages << p.page_shift) s.fault |= SPECA_STATUS_BAD_PAGE;
     if (s.fault) s.n = 0;
-    s.ct = s.fault ? 0 : (s.len + C::N - 1) / C::N;
+    s.ct = s.fault ? 0 : int((uint32_t(s.len) + C::N - 1) / C::N);           // (lengths go up to 2^31 - 1)
     return s;
 }
 // draft nodes that the rows of row tile m can see
@@ -252,15 +252,15 @@ template <class C> struct Cta {
         uint32_t n = 0;
         for (uint32_t seg = 0; ok && record(seg, r); ++seg) {
             const int32_t *table = p.page_table + size_t(r.b) * p.max_pages;
-            const int pages = (r.len + (1 << p.page_shift) - 1) >> p.page_shift;
-            int window = (r.t0 * N) >> p.page_shift;         // 32 entries of the table, one a lane, and the 32 behind them
+            const int pages = int((uint32_t(r.len) + (1u << p.page_shift) - 1u) >> p.page_shift);
+            int window = r.t0 < r.ct ? (r.t0 * N) >> p.page_shift : 0;        // 32 entries of the table, one a lane, and the 32 behind them
             auto entries = [&](int first) { return r.t0 < r.ct && first + lane < pages ? table[first + lane] : 0; };
             int ids = entries(window), next = entries(window + 32);
 #pragma unroll 1
             for (int t = r.t0; t < r.t1; ++t, ++n) {
                 int at = 0;                                  // this lane's page of the tile, as a row of the map
                 if (t < r.ct) {
-                    const int page = (t * N + lane * box_rows) >> p.page_shift, first = (t * N) >> p.page_shift;
+                    const int page = int((uint32_t(t * N) + uint32_t(lane * box_rows)) >> p.page_shift), first = (t * N) >> p.page_shift;
                     if (first >= window + 32) {
                         window = first;
                         ids = next;
