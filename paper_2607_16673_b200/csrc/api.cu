@@ -179,6 +179,10 @@ void speca_test_withhold_first_load(int on)
     attend_set_withhold(on);
 }
 
+/* Test hook, deliberately absent from speca.h: the next tree attentions take their shared memory for misaligned, which
+ * they refuse to work in (SPECA_STATUS_TIMEOUT). */
+void speca_test_misplace_shared_memory(int on) { attend_set_misplaced(on); }
+
 /* Test hook, deliberately absent from speca.h: speca_commit hands accepted paths of six to eight nodes to its
  * tensor-core kernel only when the batch is large enough for throughput to matter (n 16-row tiles per resident
  * warp; default 128).  n = 0 makes every batch of a supported shape take it, n < 0 restores the default. */

@@ -169,8 +169,8 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
     extern __shared__ __align__(1024) uint8_t smem[];
     Cta<C> x(p, plan, smem);
     const uint32_t sbase = x.sbase;
-    if (sbase & 1023u) {                                     // never expected; refuse to run rather than corrupt
-        if (threadIdx.x == 0) atomicOr(p.status, SPECA_STATUS_TIMEOUT);
+    if ((sbase & 1023u) != 0u || p.misplaced) {              // never expected; refuse to run rather than corrupt
+        x.refuse();
         return;
     }
     auto bar = [&](int i) { return x.bar(i); };
@@ -618,10 +618,7 @@ attend_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, int32_
     }
     tc_fence_before();
     __syncthreads();
-    if (threadIdx.x == 0 && *abort_flag) {
-        atomicOr(p.status, SPECA_STATUS_TIMEOUT);
-        plan.join[cta].parts = 0;
-    }
+    if (*abort_flag) x.refuse();
     if (warp == SOFT + 1) {
         tc_fence_after();
         tmem_dealloc(tmem, kTmemCols);
@@ -802,13 +799,15 @@ size_t attend_workspace_bytes(const speca_attn_dims *d)
     return align256(sizeof(Join) * kMaxCtas) + 2 * kMaxCtas * slot_bytes(unit_rows(d->max_nodes, d->heads / d->kv_heads, d->d_head), d->d_head);
 }
 
-static int g_withhold_first_load = 0;
+static int g_withhold_first_load = 0, g_misplaced = 0;
 void attend_set_withhold(int on) { g_withhold_first_load = on; }
+void attend_set_misplaced(int on) { g_misplaced = on; }
 
 int launch_attend(const AttnParams &call, int d_head, cudaStream_t st)
 {
     AttnParams p = call;
     p.withhold_first_load = g_withhold_first_load;
+    p.misplaced = g_misplaced;
     if (d_head == 64) return launch_width<64>(p, st);
     if (d_head == 128) return launch_width<128>(p, st);
     return launch_width<256>(p, st);

@@ -196,6 +196,13 @@ template <class C> struct Cta {
     {
     }
     __device__ __forceinline__ uint32_t bar(int i) const { return sbase + C::OffBars + 8u * uint32_t(i); }
+    // This CTA gives up: said in the status, and nothing of it is joined (what stands in the workspace is not a record of this call).
+    __device__ __forceinline__ void refuse() const
+    {
+        if (threadIdx.x != 0) return;
+        atomicOr(p.status, SPECA_STATUS_TIMEOUT);
+        plan.join[blockIdx.x].parts = 0;
+    }
     // by the first warp, before the barriers' fence
     __device__ __forceinline__ void init(int consumers, int empties)
     {

@@ -81,8 +81,8 @@ attend_few_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, in
     constexpr int KB = C::KB, KW = C::KW, OC = C::OC, KS = C::KS, VS = C::VS;
     extern __shared__ __align__(1024) uint8_t smem[];
     Cta<C> x(p, plan, smem);
-    if (x.sbase & 1023u) {                                   // never expected; refuse to run rather than corrupt
-        if (threadIdx.x == 0) atomicOr(p.status, SPECA_STATUS_TIMEOUT);
+    if ((x.sbase & 1023u) != 0u || p.misplaced) {            // never expected; refuse to run rather than corrupt
+        x.refuse();
         return;
     }
     const int warp = x.warp, lane = x.lane, cta = blockIdx.x;
@@ -332,10 +332,7 @@ attend_few_kernel(const __grid_constant__ Maps maps, AttnParams p, Plan plan, in
         while (global_timer_ns() - t0 < 200000ull) __nanosleep(1000);
     }
     __syncthreads();
-    if (threadIdx.x == 0 && *x.abort_flag) {
-        atomicOr(p.status, SPECA_STATUS_TIMEOUT);
-        plan.join[cta].parts = 0;
-    }
+    if (*x.abort_flag) x.refuse();
 }
 
 std::atomic<bool> g_opted_in[64];                            // per device: shared memory of every instantiation

@@ -13,6 +13,7 @@ struct AttnParams {
     float scale;
     int32_t max_nodes, page_shift, n_pages, max_pages, max_depth;
     int32_t withhold_first_load;    // failure-detection test: CTA 0 never requests its first keys
+    int32_t misplaced;              // failure-detection test: CTAs take their shared memory for misaligned
     const __nv_bfloat16 *q, *k, *v;
     __nv_bfloat16 *k_cache, *v_cache, *o;
     const int32_t *node_offsets, *parent, *page_table, *kv_len, *path_idx, *path_len;
@@ -30,6 +31,7 @@ struct NormParams {
 
 size_t attend_workspace_bytes(const speca_attn_dims *d);
 void attend_set_withhold(int on);
+void attend_set_misplaced(int on);
 int launch_attend(const AttnParams &p, int d_head, cudaStream_t st);
 int launch_norm_rope(const AttnParams &p, const NormParams &n, int d_head, cudaStream_t st);
 int launch_commit_kv(const AttnParams &p, int d_head, int32_t *kv_len_out, cudaStream_t st);
