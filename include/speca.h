@@ -385,7 +385,7 @@ typedef struct speca_attn_dims {
     int32_t heads;       /* query heads, a multiple of kv_heads, at most 4096        */
     int32_t kv_heads;    /* key and value heads >= 1                                  */
     int32_t d_head;      /* 64, 128 or 256                                            */
-    float   scale;       /* softmax(scale * q k^T), > 0; usually d_head ^ -1/2        */
+    float   scale;       /* softmax(scale * q k^T), > 0, at most 2.3e38; usually d_head ^ -1/2 */
     int32_t max_nodes;   /* draft nodes (or prompt tokens) per sequence and call      */
     int32_t page_size;   /* rows of a page: 16, 32, 64, 128 or 256                    */
     int32_t n_pages;     /* pages of the pool                                         */

@@ -492,7 +492,8 @@ int speca_attend_tree(const speca_attn_dims *dims, const uint16_t *q, const uint
     if (rc != SPECA_OK) return rc;
     if (!node_offsets || !k_cache || !v_cache || !page_table || !kv_len || !status_word) return SPECA_ERR_NULL;
     if (total_nodes > 0 && (!q || !k || !v || !o)) return SPECA_ERR_NULL;
-    if (!(dims->scale > 0.f) || !(dims->scale < 3.4e38f)) return SPECA_ERR_RANGE;
+    // (the kernels multiply by scale log2(e), which has to be finite)
+    if (!(dims->scale > 0.f) || !(dims->scale * 1.4426950408889634f <= 3.402823466e38f)) return SPECA_ERR_RANGE;
     rc = check_attn_draft(dims, total_nodes, parent_or_null);
     if (rc != SPECA_OK) return rc;
     if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(k_cache) || misaligned(v_cache) || misaligned(o)) return SPECA_ERR_ALIGN;
