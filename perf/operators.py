@@ -141,6 +141,13 @@ def _on(x, dtype=torch.int32):
 
 
 def prepare(case, seed):
+    s = _inputs(case, seed)
+    if own:
+        _set_up(s)
+    return s
+
+
+def _inputs(case, seed):
     L, B, Hq, Hkv, d, page = (case[k] for k in ("L", "B", "Hq", "Hkv", "d", "page"))
     rng = np.random.RandomState(seed % (1 << 31))
     gen = torch.Generator(DEV).manual_seed(seed)
@@ -149,8 +156,8 @@ def prepare(case, seed):
     T = int(offs[-1])
     tree = case["kind"] == "tree"
     parents = [_tree(int(n), rng) for n in nodes] if tree else None
-    s = dict(case=case, T=T, offs=_on(offs), kv_len=_on(lens), status=torch.zeros(1, dtype=torch.int32, device=DEV),
-             parent=_on(np.concatenate(parents)) if tree else None)
+    s = dict(case=case, T=T, max_nodes=int(nodes.max()), offs=_on(offs), kv_len=_on(lens),
+             status=torch.zeros(1, dtype=torch.int32, device=DEV), parent=_on(np.concatenate(parents)) if tree else None)
 
     def normal(*shape, std=1.0):
         return torch.empty(shape, dtype=torch.bfloat16, device=DEV).normal_(0.0, std, generator=gen)
@@ -302,15 +309,21 @@ def _plain_copy(s):
 # ---------------------------------------------------------------------------------------------------------------
 # the framework's calls
 # ---------------------------------------------------------------------------------------------------------------
-def _own(s):
+def _set_up(s):
+    # shapes and workspace, which a program makes once and keeps from call to call
     from paper_2607_16673_b200 import binding as speca
     c = s["case"]
-    if "dims" not in s:                     # what a program sets up once
-        s["dims"] = speca.AttnDims(c["L"], c["B"], c["Hq"], c["Hkv"], c["d"], scale=c["d"] ** -0.5,
-                                   max_nodes=int(_sizes(c)[1].max()), page_size=c["page"], n_pages=s["n_pages"],
-                                   max_pages=s["max_pages"])
-        s["ws"] = speca.alloc_attn_workspace(s["dims"]) if c["op"] == "attend" else None
-    D = s["dims"]
+    s["dims"] = speca.AttnDims(c["L"], c["B"], c["Hq"], c["Hkv"], c["d"], scale=c["d"] ** -0.5,
+                               max_nodes=s["max_nodes"], page_size=c["page"], n_pages=s["n_pages"],
+                               max_pages=s["max_pages"])
+    s["ws"] = speca.alloc_attn_workspace(s["dims"]) if c["op"] == "attend" else None
+
+
+def _own(s):
+    from paper_2607_16673_b200 import binding as speca
+    if "dims" not in s:                     # inputs that were made for the plain forms
+        _set_up(s)
+    c, D = s["case"], s["dims"]
     if c["op"] == "attend":
         speca.attend_tree(D, s["q"], s["k"], s["v"], s["offs"], s["T"], s["parent"], s["k_cache"], s["v_cache"],
                           s["table"], s["kv_len"], s["o"], s["ws"], s["status"])
