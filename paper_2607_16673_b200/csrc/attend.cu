@@ -3,7 +3,10 @@
 // For a key head the rows of a product are the (node, query head) pairs of a sequence that share it, up to 128 a tile; the
 // columns are keys.  Per tile of N keys:  S = Q K^T (both operands in shared memory, K as its pages lie), the weights
 // P = exp2((S - m) scale log2 e) with a running maximum m, rounded to bf16 and written over S in TMEM, and O += P V with P
-// from TMEM and V as its pages lie (keys along the rows: an MN-major operand).  O stays in TMEM; it is scaled down only when
+// from TMEM and V as its pages lie (keys along the rows: an MN-major operand).  The rounding of P is the tensor core's: both operands
+// of a product have one type, and V is bf16.  It adds 1.5e-3 of the output's norm to the 1.7e-3 of the output's own rounding
+// (2.2e-3 in all against 64 bits); the remainder of P in a second product would take it away for half as many products again.
+// The sum of weights is of the unrounded ones.  O stays in TMEM; it is scaled down only when
 // a row's maximum has grown by more than kSlack, so that a weight is at most 2^kSlack and the sum of weights, kept in fp32,
 // and O are in the same scale whatever that scale is.
 //
@@ -23,7 +26,9 @@ constexpr float kSlack = 8.f;            // binary digits a maximum may grow by 
 // D <= 128: two softmax groups of 128 rows, each with an O of its own.  A unit of at most 128 rows has its even key tiles in one
 // and the odd ones in the other, joined at the end; a larger one has a row tile in each, over the same keys.  D = 256: O alone
 // takes half of TMEM, and there is one group; its queries have a quarter of TMEM, so that a tile's scores do not read 64 KB of
-// shared memory once more and the rings have room for one tile more.  P takes the first half of the columns of its S.  One warp asks for scores, another
+// shared memory once more and the rings have room for one tile more.  Of the 1880 cycles of a tile (16 trees of 40..64 nodes behind
+// 2001..30000) the softmax warps work 1310, one on each scheduler; the product warp waits 920 for weights and 640 for values, the
+// score warp 540 for keys.  P takes the first half of the columns of its S.  One warp asks for scores, another
 // for the products with V, so that neither's waits hold the other up (a loop over one item takes 1200 cycles beside its 12
 // products where one warp does both).
 // MANY: units of more than 128 rows.  Products and softmax bound these: tiles of 64 keys leave room for a second buffer of S in

@@ -20,7 +20,7 @@ struct Rec {
     int l, b, hk, base;
     int n, len, row0, rows;
     int t0, t1, ct, nodes;                                   // nodes: draft nodes the unit's rows can see (0 .. nodes-1)
-    int slot, index, pad0, pad1;                             // slot: -1 the whole unit, 0 / 1 where its sums go
+    int slot, pad0, pad1, pad2;                              // slot: -1 the whole unit, 0 / 1 where its sums go
 };
 static_assert(sizeof(Rec) == 64, "record");
 
@@ -219,7 +219,7 @@ template <class C> struct Cta {
         if (!(ok = wait_fast(bar(C::kRecFull + (s % kRecords)), (s / kRecords) & 1, abort_flag))) return false;
         const int4 *src = reinterpret_cast<const int4 *>(smem + C::OffRec) + 4 * (s % kRecords);
         const int4 a = src[0], b = src[1], c = src[2], d = src[3];
-        r = Rec{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w, c.x, c.y, c.z, c.w, d.x, d.y, 0, 0};
+        r = Rec{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w, c.x, c.y, c.z, c.w, d.x, 0, 0, 0};
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(C::kRecEmpty + (s % kRecords)));
         return r.rows > 0;
