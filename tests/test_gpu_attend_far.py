@@ -1,4 +1,4 @@
-"""Tree attention behind contexts of nearly 2^31 rows, the most that a page table may describe."""
+"""Contexts of nearly 2^31 rows, the most that a page table may describe: tree attention behind them, commits to their end."""
 import pytest
 import torch
 
@@ -47,3 +47,27 @@ def test_lengths_next_to_the_limit(H, d, n):
         far = rows.repeat(d // 4) / (length + i + 1)
         for at, want in ((i, short), (n + i, far)):
             assert bool(((o[0, at].double() - want).abs() <= (BF16 + 2.0 ** -14) * want).all()), (at, i)
+
+
+@pytest.mark.parametrize("extra,in_place", [(0, False), (0, True), (1, False), (1, True)])
+def test_commit_up_to_the_limit(extra, in_place):
+    """Four rows appended where four are left, and where three are: then nothing is, and it is said."""
+    page, max_pages, d = 32, (1 << 26) - 1, 64
+    length = max_pages * page - 4 + extra
+    if torch.cuda.mem_get_info()[0] < 2 << 30:
+        pytest.skip("needs 2 GB of device memory")
+    cache = [torch.zeros(1, 2, 1, page, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    rec = [torch.empty(1, 4, 1, d, dtype=torch.bfloat16, device="cuda").normal_() for _ in range(2)]
+    table = torch.zeros(1, max_pages, dtype=torch.int32, device="cuda")
+    table[0, -1] = 1
+    kv_len, status = dev([length]), dev([0])
+    out = kv_len if in_place else torch.zeros_like(kv_len)
+    dims = speca.AttnDims(1, 1, 1, 1, d, 1.0, 4, page, 2, max_pages)
+    speca.commit_kv(dims, *cache, table, kv_len, *rec, dev([0, 4]), 4, None, None, None, out, status)
+    torch.cuda.synchronize()
+    for x, y in zip(cache, rec):
+        assert int(x[0, 0].count_nonzero()) == 0
+        assert torch.equal(x[0, 1, 0, -4:], torch.zeros_like(y[0, :, 0]) if extra else y[0, :, 0])
+        assert int(x[0, 1, 0, :-4].count_nonzero()) == 0
+    assert out.tolist() == [length if extra else length + 4]
+    assert int(status) == (speca.STATUS_BAD_PAGE if extra else 0)
